@@ -278,6 +278,124 @@ evomoe_status evomoe_diversify(evomoe_ctx* ctx, const evomoe_shape* shape,
                                uint64_t seed, float mask_ratio,
                                void* W1, float* b1, void* W2, float* b2);
 
+/* ---- the operators of an MoE block beside the DTS gate -------------------------------------------
+ * A pre-norm block around this layer is   norm -> gate logits -> top-k gate -> dispatch -> experts -> combine:
+ * the calls below are the ones that the DTS-gate path has no part of.  They take the same shape, context and
+ * conventions, and their outputs are the inputs of evomoe_dispatch, evomoe_expert_ffn, evomoe_combine and
+ * evomoe_balance_loss.  They run on the context's device whatever device is current, allocate nothing (but for
+ * evomoe_gate_logits, whose split copy of W_g grows with d as evomoe_dts_gate's) and may be captured into a HIP graph;
+ * calls that may overlap in time need contexts and workspaces of their own. */
+
+/* Gate logits:  logits[t,:] = x_t . W_g + b_g.
+ *   in : x [T,d] elem; Wg [d,E] f32; bg [E] f32 or NULL.   out: logits [T,E] f32.
+ * F and P_cap of the shape are not used. */
+evomoe_status evomoe_gate_logits(evomoe_ctx* ctx, const evomoe_shape* shape,
+                                 const void* x, const float* Wg, const float* bg, float* logits);
+
+/* Backward of the logits:  dWg = x^T dlogits;  dbg = sum_t dlogits_t;  dx = dx_in + dlogits W_g^T.
+ *   in : dlogits [T,E] f32, x, Wg as in the forward; dx_in [T,d] elem (what else flows into x, for instance the output of
+ *        evomoe_dispatch_bwd; NULL = 0).
+ *   out: dWg [d,E] f32, dbg [E] f32 (may be NULL), dx [T,d] elem; dx may be dx_in itself.
+ *   workspace: at least evomoe_workspace_bytes(shape) bytes. */
+evomoe_status evomoe_gate_logits_bwd(evomoe_ctx* ctx, const evomoe_shape* shape,
+                                     const float* dlogits, const void* x, const float* Wg, const void* dx_in,
+                                     float* dWg, float* dbg, void* dx,
+                                     void* workspace, size_t workspace_bytes);
+
+/* Top-k gate.  Of a token's scores s = softmax(z) or sigmoid(z), z its logits, the k experts with the largest keys are
+ * selected; the key of expert i is s_i + balance_bias_i.  With groups > 1 the experts are `groups` runs of E / groups;
+ * a group is worth the sum of its group_keys largest keys (that are not -inf), and only experts of the top_groups most valuable groups are
+ * selected.  Ties go to the lowest index.  The bias decides the selection alone: the weight of a selected expert is
+ *     w_i = scale * s_i        or, renormalised,     w_i = scale * s_i / sum of s over the token's selected experts.
+ * Keys are compared as 64-bit values of the float32 logits (with no bias and one group, the logits themselves are), so
+ * the selection depends neither on the rounding of an exponential nor on the batch that a token is in.
+ *  - A logit or a bias of -inf takes the expert out: it is not selected, and a logit of -inf has the score 0.  A token with fewer
+ *    than k experts left selects those, one with none (padding) selects nothing: k_s = 0, and the layer's output is 0.
+ *  - A NaN key ranks above every number, so that a NaN reaches the output; so do the NaNs of a softmax over +inf.  */
+typedef enum { EVOMOE_SOFTMAX = 0, EVOMOE_SIGMOID = 1 } evomoe_score;
+typedef struct {
+    int32_t k;             /* 1 <= k <= top_groups * E / groups */
+    int32_t score;         /* evomoe_score */
+    int32_t groups;        /* >= 1, divides E */
+    int32_t top_groups;    /* 1 .. groups */
+    int32_t group_keys;    /* 1 or 2 */
+    int32_t renormalise;   /* 0 or 1 */
+    float scale;           /* finite, > 0 */
+} evomoe_topk;
+/*   in : logits [T,E] f32; balance_bias [E] f32 or NULL.
+ *   out: scores [T,E] f32 (may be NULL; evomoe_balance_loss takes them in place of g'); gate_w [T,E] f32 = w where selected,
+ *        else 0; mask_bits [T] u64; counts [E] i32; k_per_token [T] i32 (may be NULL); block_hist [ceil(T/256), E] i32 (may
+ *        be NULL): all as evomoe_dts_gate writes them, for evomoe_dispatch (whose `scores` is gate_w here).
+ * d, F and P_cap of the shape are not used. */
+evomoe_status evomoe_topk_gate(evomoe_ctx* ctx, const evomoe_shape* shape, const evomoe_topk* topk,
+                               const float* logits, const float* balance_bias,
+                               float* scores, float* gate_w, uint64_t* mask_bits,
+                               int32_t* counts, int32_t* k_per_token, int32_t* block_hist);
+
+/* Backward of the top-k gate, its selection a constant:  with w^ = w / scale, G_i the gradient of the weight of expert i
+ * (dG_pairs at the token's selected experts, 0 elsewhere) and c_i = loss_scale * dscore_coef_i for EVERY expert,
+ *     u_i = scale * w^_i (G_i - sum_j G_j w^_j)  if renormalised,  scale * s_i G_i  if not  (selected experts, else 0);
+ *     v_i = u_i + s_i c_i;
+ *     softmax:  dz_i = v_i - s_i sum_j v_j;       sigmoid:  dz_i = v_i (1 - s_i).
+ *   in : dG_pairs [P_cap] f32, tok_off, tok_rows (as written by evomoe_dispatch and evomoe_combine_bwd), logits and mask_bits
+ *        of the forward, dscore_coef [E] f32 (as written by evomoe_balance_loss) or NULL.
+ *   out: dlogits [T,E] f32. */
+evomoe_status evomoe_topk_gate_bwd(evomoe_ctx* ctx, const evomoe_shape* shape, const evomoe_topk* topk,
+                                   const float* dG_pairs, const int32_t* tok_off, const int32_t* tok_rows,
+                                   const float* logits, const uint64_t* mask_bits,
+                                   const float* dscore_coef, float loss_scale, float* dlogits);
+
+/* 8-bit values (MX): e4m3 elements, and for 32 neighbours of a row one e8m0 scale byte b, which stands for 2^(b - 127).
+ * The scale is the smallest power of two, 2^-127 at least, with which the largest of the 32 magnitudes stays within 448;
+ * elements are rounded to nearest even.  An infinity or a NaN becomes a NaN and has no part in the scale.  A matrix
+ * [rows, n] is elements [rows, n] and scales [rows, n / 32], both dense; n is a multiple of 32. */
+
+/* Residual addition and root-mean-square norm:  h = x + residual, rounded to elem;
+ *     rstd_t = 1 / sqrt(mean_j h_tj^2 + eps);     y_tj = h_tj rstd_t gamma_j.
+ *   in : x [T,d] elem; residual [T,d] elem or NULL (h = x); gamma [d] f32; eps > 0.
+ *   out: h [T,d] elem (may be NULL, and may be x or residual itself); y [T,d] elem (may be NULL, and may be x or residual);
+ *        rstd [T] f32 (may be NULL; the backward reads it); q [T,d] e4m3 and q_scale [T,d/32] e8m0 (both or neither; d a
+ *        multiple of 32): y in 8 bits, from the float32 values that y is rounded from.
+ * One of h, y, q at least; no two outputs may be the same.  The squares are summed in float32: rows with values above 1e18 overflow.
+ * E, F and P_cap of the shape are not used. */
+evomoe_status evomoe_add_rmsnorm(evomoe_ctx* ctx, const evomoe_shape* shape,
+                                 const void* x, const void* residual, const float* gamma, float eps,
+                                 void* h, void* y, float* rstd, void* q, uint8_t* q_scale);
+
+/* Backward of the norm:  with n_tj = h_tj rstd_t,
+ *     dx_tj = dh_tj + rstd_t (gamma_j dy_tj - n_tj mean_i(gamma_i dy_ti n_ti));     dgamma_j = sum_t dy_tj n_tj.
+ * dx is the gradient of x and of the residual alike.
+ *   in : dy [T,d] elem; dh [T,d] elem (what flows into h besides; NULL = 0); h [T,d] (x where there was no residual), gamma,
+ *        rstd as in the forward.
+ *   out: dx [T,d] elem (may be dy or dh itself); dgamma [d] f32 (may be NULL).
+ *   workspace: at least evomoe_workspace_bytes(shape) bytes (not read or checked without dgamma). */
+evomoe_status evomoe_add_rmsnorm_bwd(evomoe_ctx* ctx, const evomoe_shape* shape,
+                                     const void* dy, const void* dh, const void* h, const float* gamma,
+                                     const float* rstd, void* dx, float* dgamma,
+                                     void* workspace, size_t workspace_bytes);
+
+/* A matrix in 8 bits: src [rows, cols] of type dtype -> q [rows, cols] e4m3, q_scale [rows, cols/32] e8m0.  Weights are
+ * converted once (W1 as [E*F, d], W2 as [E*d, F]), rows of x where no norm has done it.  cols a multiple of 32. */
+evomoe_status evomoe_quantize_mx8(evomoe_ctx* ctx, int64_t rows, int64_t cols, int dtype,
+                                  const void* src, void* q, uint8_t* q_scale);
+
+/* Expert FFNs forward in 8 bits, for serving a bf16 layer: evomoe_expert_ffn with x, W1, W2 and act(H) as 8-bit values, products
+ * on the scaled matrix instructions, sums, biases and activation in float32.  act(H) is converted in float32 and stays in
+ * the workspace.
+ *   in : x_q [T,d], x_scale [T,d/32], gathered through pair_token [P_cap], or, if pair_token == NULL, permuted rows
+ *        [P_cap,d]; expert_offsets [E+1]; W1_q [E,F,d], W1_scale [E,F,d/32], b1 [E,F] f32 (NULL = 0), W2_q [E,d,F],
+ *        W2_scale [E,d,F/32], b2 [E,d] f32 (NULL = 0).
+ *   out: O [P_cap,d] bf16, rows below P only.
+ *   workspace: at least evomoe_workspace_bytes_mx8(shape) bytes (evomoe_workspace_bytes is more than that).
+ * Limits: dtype bf16; d and F multiples of 32; T*max(d,F) and d*F below 2^32. */
+size_t evomoe_workspace_bytes_mx8(const evomoe_shape* shape);
+evomoe_status evomoe_expert_ffn_mx8(evomoe_ctx* ctx, const evomoe_shape* shape,
+                                    const void* x_q, const uint8_t* x_scale,
+                                    const int32_t* pair_token, const int32_t* expert_offsets,
+                                    const void* W1_q, const uint8_t* W1_scale, const float* b1,
+                                    const void* W2_q, const uint8_t* W2_scale, const float* b2,
+                                    void* O, void* workspace, size_t workspace_bytes);
+
 /* Copies P to the host and reports a pending capacity overflow.  The only synchronising call. */
 evomoe_status evomoe_num_pairs(evomoe_ctx* ctx, const int64_t* num_pairs, int64_t* num_pairs_host);
 
@@ -299,6 +417,8 @@ typedef enum {
     EVOMOE_K_FFN_BWD_DX, EVOMOE_K_FFN_BWD_DW2, EVOMOE_K_FFN_BWD_DW1, EVOMOE_K_FFN_BWD_DB,
     EVOMOE_K_DISPATCH_BWD, EVOMOE_K_GATE_BWD_DZ, EVOMOE_K_GATE_BWD_MAIN, EVOMOE_K_GATE_BWD_REDUCE,
     EVOMOE_K_BALANCE_LOSS, EVOMOE_K_DIVERSIFY,
+    EVOMOE_K_GATE_LOGITS, EVOMOE_K_TOPK_GATE, EVOMOE_K_TOPK_GATE_BWD, EVOMOE_K_ADD_RMSNORM, EVOMOE_K_ADD_RMSNORM_BWD,
+    EVOMOE_K_QUANTIZE_MX8, EVOMOE_K_FFN_MX8_GEMM1, EVOMOE_K_FFN_MX8_GEMM2,
     EVOMOE_K_COUNT, EVOMOE_K_ALL = -2, EVOMOE_K_NONE = -1
 } evomoe_kernel_id;
 evomoe_status evomoe_profile_select(evomoe_ctx* ctx, int kernel_id);

@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libevomoe.so")   # tests and tools may point thi
 
 EVOMOE_F32, EVOMOE_BF16 = 0, 1
 EVOMOE_RELU, EVOMOE_GELU_ERF = 0, 1
+EVOMOE_SOFTMAX, EVOMOE_SIGMOID = 0, 1
 EVOMOE_OK, EVOMOE_EINVAL, EVOMOE_EUNSUPPORTED, EVOMOE_ECAPACITY, EVOMOE_EWORKSPACE, EVOMOE_EHIP = 0, -1, -2, -3, -4, -5
 EVOMOE_ESTATIC = -6
 
@@ -29,11 +30,15 @@ ENTRY_POINTS = (
     "evomoe_dts_gate_top1", "evomoe_balance_loss", "evomoe_dts_gate_bwd_balance",
     "evomoe_workspace_bytes_recompute", "evomoe_expert_ffn_bwd_recompute", "evomoe_schedule",
     "evomoe_hint_pairs", "evomoe_diversify", "evomoe_dispatch_static",
+    "evomoe_gate_logits", "evomoe_gate_logits_bwd", "evomoe_topk_gate", "evomoe_topk_gate_bwd",
+    "evomoe_add_rmsnorm", "evomoe_add_rmsnorm_bwd", "evomoe_quantize_mx8", "evomoe_workspace_bytes_mx8",
+    "evomoe_expert_ffn_mx8",
 )
 
 KERNEL_IDS = ("gate", "dispatch_hist", "dispatch_scatter", "ffn_gemm1", "ffn_gemm2", "combine", "combine_bwd",
               "ffn_bwd_dh", "ffn_bwd_dx", "ffn_bwd_dw2", "ffn_bwd_dw1", "ffn_bwd_db", "dispatch_bwd",
-              "gate_bwd_dz", "gate_bwd_main", "gate_bwd_reduce", "balance_loss", "diversify")
+              "gate_bwd_dz", "gate_bwd_main", "gate_bwd_reduce", "balance_loss", "diversify", "gate_logits", "topk_gate",
+              "topk_gate_bwd", "add_rmsnorm", "add_rmsnorm_bwd", "quantize_mx8", "ffn_mx8_gemm1", "ffn_mx8_gemm2")
 EVOMOE_K_ALL, EVOMOE_K_NONE = -2, -1
 
 
@@ -51,6 +56,12 @@ class Phase(ctypes.Structure):
 class Shape(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int32), ("d", ctypes.c_int32), ("E", ctypes.c_int32), ("F", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("P_cap", ctypes.c_int64)]
+
+
+class TopK(ctypes.Structure):
+    """evomoe_topk: how evomoe_topk_gate selects and weighs experts (make_topk)."""
+    _fields_ = [("k", ctypes.c_int32), ("score", ctypes.c_int32), ("groups", ctypes.c_int32), ("top_groups", ctypes.c_int32),
+                ("group_keys", ctypes.c_int32), ("renormalise", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 _lib = None
@@ -90,11 +101,23 @@ def lib() -> ctypes.CDLL:
         L.evomoe_expert_ffn_bwd_recompute.argtypes = [vp, sp] + [vp] * 14 + [i32, vp, sz]
         L.evomoe_hint_pairs.argtypes = [vp, ctypes.c_int64]
         L.evomoe_diversify.argtypes = [vp, sp, vp, vp, vp, vp, ctypes.c_uint64, f32, vp, vp, vp, vp]
+        tp, i64 = ctypes.POINTER(TopK), ctypes.c_int64
+        L.evomoe_gate_logits.argtypes = [vp, sp] + [vp] * 4
+        L.evomoe_gate_logits_bwd.argtypes = [vp, sp] + [vp] * 8 + [sz]
+        L.evomoe_topk_gate.argtypes = [vp, sp, tp] + [vp] * 8
+        L.evomoe_topk_gate_bwd.argtypes = [vp, sp, tp] + [vp] * 6 + [f32, vp]
+        L.evomoe_add_rmsnorm.argtypes = [vp, sp, vp, vp, vp, f32] + [vp] * 5
+        L.evomoe_add_rmsnorm_bwd.argtypes = [vp, sp] + [vp] * 8 + [sz]
+        L.evomoe_quantize_mx8.argtypes = [vp, i64, i64, i32, vp, vp, vp]
+        L.evomoe_workspace_bytes_mx8.argtypes = [sp]
+        L.evomoe_workspace_bytes_mx8.restype = sz
+        L.evomoe_expert_ffn_mx8.argtypes = [vp, sp] + [vp] * 12 + [sz]
         L.evomoe_schedule.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, f32, f32, ctypes.POINTER(Phase)]
         L.evomoe_profile_select.argtypes = [vp, i32]
         L.evomoe_profile_read.argtypes = [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64)]
         for n in ENTRY_POINTS:
-            if n not in ("evomoe_status_string", "evomoe_workspace_bytes", "evomoe_workspace_bytes_recompute"):
+            if n not in ("evomoe_status_string", "evomoe_workspace_bytes", "evomoe_workspace_bytes_recompute",
+                         "evomoe_workspace_bytes_mx8"):
                 getattr(L, n).restype = i32
         _lib = L
     return _lib
@@ -241,6 +264,67 @@ def evomoe_expert_ffn_bwd_recompute(ctx, shape, dO, x, pair_token, expert_offset
          "evomoe_expert_ffn_bwd_recompute")
 
 
+def make_topk(k, score="softmax", groups=1, top_groups=1, group_keys=1, renormalise=True, scale=1.0) -> TopK:
+    return TopK(k, {"softmax": EVOMOE_SOFTMAX, "sigmoid": EVOMOE_SIGMOID}[score], groups, top_groups, group_keys,
+                int(renormalise), scale)
+
+
+def evomoe_gate_logits(ctx, shape, x, Wg, bg, logits):
+    _chk(lib().evomoe_gate_logits(ctx._h, ctypes.byref(shape), _p(x), _p(Wg), _p(bg), _p(logits)), "evomoe_gate_logits")
+
+
+def evomoe_gate_logits_bwd(ctx, shape, dlogits, x, Wg, dx_in, dWg, dbg, dx, workspace):
+    _chk(lib().evomoe_gate_logits_bwd(ctx._h, ctypes.byref(shape), _p(dlogits), _p(x), _p(Wg), _p(dx_in), _p(dWg),
+                                      _p(dbg), _p(dx), _p(workspace), workspace.numel() * workspace.element_size()),
+         "evomoe_gate_logits_bwd")
+
+
+def evomoe_topk_gate(ctx, shape, topk, logits, balance_bias, scores, gate_w, mask_bits, counts, k_per_token=None,
+                     block_hist=None):
+    _chk(lib().evomoe_topk_gate(ctx._h, ctypes.byref(shape), ctypes.byref(topk), _p(logits), _p(balance_bias),
+                                _p(scores), _p(gate_w), _p(mask_bits), _p(counts), _p(k_per_token), _p(block_hist)),
+         "evomoe_topk_gate")
+
+
+def evomoe_topk_gate_bwd(ctx, shape, topk, dG_pairs, tok_off, tok_rows, logits, mask_bits, dscore_coef, loss_scale,
+                         dlogits):
+    _chk(lib().evomoe_topk_gate_bwd(ctx._h, ctypes.byref(shape), ctypes.byref(topk), _p(dG_pairs), _p(tok_off),
+                                    _p(tok_rows), _p(logits), _p(mask_bits), _p(dscore_coef), loss_scale,
+                                    _p(dlogits)), "evomoe_topk_gate_bwd")
+
+
+def evomoe_add_rmsnorm(ctx, shape, x, residual, gamma, eps, h, y, rstd=None, q=None, q_scale=None):
+    _chk(lib().evomoe_add_rmsnorm(ctx._h, ctypes.byref(shape), _p(x), _p(residual), _p(gamma), eps, _p(h), _p(y),
+                                  _p(rstd), _p(q), _p(q_scale)), "evomoe_add_rmsnorm")
+
+
+def evomoe_add_rmsnorm_bwd(ctx, shape, dy, dh, h, gamma, rstd, dx, dgamma, workspace=None):
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _chk(lib().evomoe_add_rmsnorm_bwd(ctx._h, ctypes.byref(shape), _p(dy), _p(dh), _p(h), _p(gamma), _p(rstd), _p(dx),
+                                      _p(dgamma), _p(workspace), nbytes), "evomoe_add_rmsnorm_bwd")
+
+
+def evomoe_quantize_mx8(ctx, src, q, q_scale):
+    """src [..., n] float32 or bfloat16 -> q [..., n] (float8_e4m3fn), q_scale [..., n/32] (float8_e8m0fnu)."""
+    cols = src.shape[-1]
+    assert q.shape == src.shape and q_scale.shape == (*src.shape[:-1], cols // 32), "q as src, q_scale [..., n/32]"
+    dtype = {torch.float32: EVOMOE_F32, torch.bfloat16: EVOMOE_BF16}[src.dtype]
+    _chk(lib().evomoe_quantize_mx8(ctx._h, src.numel() // cols, cols, dtype, _p(src), _p(q), _p(q_scale)),
+         "evomoe_quantize_mx8")
+
+
+def evomoe_workspace_bytes_mx8(shape: Shape) -> int:
+    return int(lib().evomoe_workspace_bytes_mx8(ctypes.byref(shape)))
+
+
+def evomoe_expert_ffn_mx8(ctx, shape, x_q, x_scale, pair_token, expert_offsets, W1_q, W1_scale, b1, W2_q, W2_scale, b2,
+                          O, workspace):
+    _chk(lib().evomoe_expert_ffn_mx8(ctx._h, ctypes.byref(shape), _p(x_q), _p(x_scale), _p(pair_token),
+                                     _p(expert_offsets), _p(W1_q), _p(W1_scale), _p(b1), _p(W2_q), _p(W2_scale), _p(b2),
+                                     _p(O), _p(workspace), workspace.numel() * workspace.element_size()),
+         "evomoe_expert_ffn_mx8")
+
+
 def evomoe_schedule(iteration, T_S, T_D, tau_hi=2.0, tau_lo=0.3) -> Phase:
     ph = Phase()
     _chk(lib().evomoe_schedule(iteration, T_S, T_D, tau_hi, tau_lo, ctypes.byref(ph)), "evomoe_schedule")
@@ -291,9 +375,10 @@ class LayerParams:
 
 
 class LayerBuffers:
-    """Every output / saved tensor of one forward+backward pass, allocated once."""
+    """Every output / saved tensor of one forward+backward pass, allocated once.  mx8: a forward pass with the experts in
+    8 bits, which needs no H and A but a workspace."""
 
-    def __init__(self, shape: Shape, device="cuda", backward=True, recompute=False):
+    def __init__(self, shape: Shape, device="cuda", backward=True, recompute=False, mx8=False):
         T, d, E, F, P = shape.T, shape.d, shape.E, shape.F, shape.P_cap
         dt = torch.bfloat16 if shape.dtype == EVOMOE_BF16 else torch.float32
         z = lambda *s, dtype=dt: torch.zeros(*s, dtype=dtype, device=device)
@@ -304,11 +389,16 @@ class LayerBuffers:
         self.expert_offsets = z(E + 1, dtype=i32); self.pair_token = z(P, dtype=i32)
         self.pair_gate = z(P, dtype=f32); self.tok_off = z(T + 1, dtype=i32); self.tok_rows = z(P, dtype=i32)
         self.num_pairs = z(1, dtype=i64); self.block_hist = z((T + 255) // 256, E, dtype=i32)
-        self.H = z(P, F); self.A = z(P, F); self.O = z(P, d); self.y = z(T, d)
+        self.H, self.A = (None, None) if mx8 else (z(P, F), z(P, F))
+        self.O = z(P, d); self.y = z(T, d)
+        if mx8:
+            assert not backward, "8-bit experts: forward only"
+            self.workspace = torch.empty(evomoe_workspace_bytes_mx8(shape), dtype=torch.uint8, device=device)
+        self.logits = z(T, E, dtype=f32)                     # top-k gate only; gprime then holds its scores
         if backward:
             self.dO = z(P, d); self.dG_pairs = z(P, dtype=f32); self.dXp = z(P, d); self.dx = z(T, d)
             self.dW1 = z(E, F, d); self.dW2 = z(E, d, F); self.db1 = z(E, F, dtype=f32); self.db2 = z(E, d, dtype=f32)
-            self.dWg = z(d, E, dtype=f32); self.dbg = z(E, dtype=f32)
+            self.dWg = z(d, E, dtype=f32); self.dbg = z(E, dtype=f32); self.dlogits = z(T, E, dtype=f32)
             nbytes = evomoe_workspace_bytes_recompute(shape) if recompute else evomoe_workspace_bytes(shape)
             self.workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
             self.bal_loss = z(1, dtype=f32); self.bal_coef = z(E, dtype=f32)
@@ -328,11 +418,7 @@ def layer_forward(ctx, b: LayerBuffers, p: LayerParams, x, noise, tau, threshold
     evomoe_combine(ctx, s, b.O, b.pair_gate, b.tok_off, b.tok_rows, b.y)
 
 
-def layer_backward(ctx, b: LayerBuffers, p: LayerParams, x, dy, tau, accumulate=False, balance_alpha=None,
-                   recompute=False):
-    """balance_alpha: also evaluate the balance loss and add its gradient in the gate backward (needs
-    b.bal_loss [1] f32 and b.bal_coef [E] f32).  recompute: the FFN backward recomputes H and A (needs
-    b.workspace of evomoe_workspace_bytes_recompute bytes); b.H and b.A are then not read."""
+def _experts_backward(ctx, b, p, x, dy, accumulate, recompute):
     s = b.shape
     evomoe_combine_bwd(ctx, s, dy, b.O, b.pair_gate, b.pair_token, b.expert_offsets, b.dO, b.dG_pairs)
     if recompute:
@@ -342,6 +428,15 @@ def layer_backward(ctx, b: LayerBuffers, p: LayerParams, x, dy, tau, accumulate=
         evomoe_expert_ffn_bwd(ctx, s, b.dO, b.H, b.A, x, b.pair_token, b.expert_offsets, p.W1, p.W2,
                               dy, b.pair_gate, b.dW1, b.db1, b.dW2, b.db2, b.dXp, accumulate, b.workspace)
     evomoe_dispatch_bwd(ctx, s, b.dXp, b.tok_off, b.tok_rows, b.dx)
+
+
+def layer_backward(ctx, b: LayerBuffers, p: LayerParams, x, dy, tau, accumulate=False, balance_alpha=None,
+                   recompute=False):
+    """balance_alpha: also evaluate the balance loss and add its gradient in the gate backward (needs
+    b.bal_loss [1] f32 and b.bal_coef [E] f32).  recompute: the FFN backward recomputes H and A (needs
+    b.workspace of evomoe_workspace_bytes_recompute bytes); b.H and b.A are then not read."""
+    s = b.shape
+    _experts_backward(ctx, b, p, x, dy, accumulate, recompute)
     if balance_alpha is not None:
         evomoe_balance_loss(ctx, s, b.gprime, b.counts, float(balance_alpha), b.bal_loss, b.bal_coef)
         evomoe_dts_gate_bwd_balance(ctx, s, b.dG_pairs, b.tok_off, b.tok_rows, b.gprime, b.mask_bits, tau, x, p.Wg,
@@ -349,3 +444,64 @@ def layer_backward(ctx, b: LayerBuffers, p: LayerParams, x, dy, tau, accumulate=
     else:
         evomoe_dts_gate_bwd(ctx, s, b.dG_pairs, b.tok_off, b.tok_rows, b.gprime, b.mask_bits, tau, x, p.Wg,
                             b.dWg, b.dbg, b.dx, b.workspace)
+
+
+# ---- the same layer behind the top-k gate ---------------------------------------------------------
+
+def topk_layer_forward(ctx, b: LayerBuffers, p: LayerParams, topk: TopK, x, balance_bias=None):
+    """layer_forward with the top-k gate in place of the DTS gate: b.gprime holds the scores, b.gate_w the weights."""
+    _topk_route(ctx, b, p, topk, x, balance_bias)
+    s = b.shape
+    evomoe_expert_ffn(ctx, s, x, b.pair_token, b.expert_offsets, p.W1, p.b1, p.W2, p.b2, b.H, b.A, b.O)
+    evomoe_combine(ctx, s, b.O, b.pair_gate, b.tok_off, b.tok_rows, b.y)
+
+
+def topk_layer_backward(ctx, b: LayerBuffers, p: LayerParams, topk: TopK, x, dy, accumulate=False, balance_alpha=None,
+                        recompute=False):
+    """layer_backward behind topk_layer_forward (same arguments)."""
+    s = b.shape
+    _experts_backward(ctx, b, p, x, dy, accumulate, recompute)
+    coef = None
+    if balance_alpha is not None:
+        evomoe_balance_loss(ctx, s, b.gprime, b.counts, float(balance_alpha), b.bal_loss, b.bal_coef)
+        coef = b.bal_coef
+    evomoe_topk_gate_bwd(ctx, s, topk, b.dG_pairs, b.tok_off, b.tok_rows, b.logits, b.mask_bits, coef, 1.0, b.dlogits)
+    evomoe_gate_logits_bwd(ctx, s, b.dlogits, x, p.Wg, b.dx, b.dWg, b.dbg, b.dx, b.workspace)
+
+
+def _topk_route(ctx, b, p, topk, x, balance_bias):
+    s = b.shape
+    evomoe_gate_logits(ctx, s, x, p.Wg, p.bg, b.logits)
+    evomoe_topk_gate(ctx, s, topk, b.logits, balance_bias, b.gprime, b.gate_w, b.mask_bits, b.counts, b.k, b.block_hist)
+    evomoe_dispatch(ctx, s, b.mask_bits, b.gate_w, b.expert_offsets, b.pair_token, b.pair_gate, b.tok_off, b.tok_rows,
+                    b.num_pairs, block_hist=b.block_hist)
+
+
+# ---- serving with experts in 8 bits ----------------------------------------------------------------
+
+class Mx8Experts:
+    """The experts' weights in 8 bits, converted once."""
+
+    def __init__(self, ctx, p: LayerParams):
+        self.W1, self.W1_scale = mx8_empty(p.W1.shape, p.W1.device)
+        self.W2, self.W2_scale = mx8_empty(p.W2.shape, p.W2.device)
+        self.b1, self.b2 = p.b1, p.b2
+        evomoe_quantize_mx8(ctx, p.W1, self.W1, self.W1_scale)
+        evomoe_quantize_mx8(ctx, p.W2, self.W2, self.W2_scale)
+
+
+def mx8_empty(shape, device="cuda"):
+    """An 8-bit matrix: elements [..., n] and scales [..., n/32]."""
+    return (torch.empty(*shape, dtype=torch.float8_e4m3fn, device=device),
+            torch.empty(*shape[:-1], shape[-1] // 32, dtype=torch.float8_e8m0fnu, device=device))
+
+
+def topk_layer_forward_mx8(ctx, b: LayerBuffers, p: LayerParams, topk: TopK, experts: Mx8Experts, x, x_q, x_scale,
+                           balance_bias=None):
+    """topk_layer_forward with the experts in 8 bits: x goes to the gate, x_q and x_scale (as evomoe_add_rmsnorm or
+    evomoe_quantize_mx8 write them) to the experts.  b: LayerBuffers(shape, backward=False, mx8=True)."""
+    _topk_route(ctx, b, p, topk, x, balance_bias)
+    s = b.shape
+    evomoe_expert_ffn_mx8(ctx, s, x_q, x_scale, b.pair_token, b.expert_offsets, experts.W1, experts.W1_scale, experts.b1,
+                          experts.W2, experts.W2_scale, experts.b2, b.O, b.workspace)
+    evomoe_combine(ctx, s, b.O, b.pair_gate, b.tok_off, b.tok_rows, b.y)

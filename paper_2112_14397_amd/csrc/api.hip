@@ -35,6 +35,35 @@ evomoe_status check_ffn_shape(const evomoe_shape* s) {
     return EVOMOE_OK;
 }
 
+// Limits of the 8-bit expert FFN: bf16 layers, whole groups of 32, 32-bit byte offsets inside a tile's operands.
+evomoe_status check_mx8_shape(const evomoe_shape* s) {
+    if (evomoe_status st = check_shape(s); st != EVOMOE_OK) return st;
+    const int64_t lim = (int64_t)1 << 32, wide = s->d > s->F ? s->d : s->F;
+    if (s->dtype != EVOMOE_BF16 || s->d % 32 || s->F % 32) return EVOMOE_EUNSUPPORTED;
+    if ((int64_t)s->T * wide >= lim || (int64_t)s->d * s->F >= lim) return EVOMOE_EUNSUPPORTED;
+    return EVOMOE_OK;
+}
+
+// Launches of the calls behind it go to the context's device, whatever device is current in the calling thread.
+struct OnDevice {
+    int before = -1, device;
+    bool ok;
+    explicit OnDevice(const Ctx& c) : device(c.device) {
+        ok = hipGetDevice(&before) == hipSuccess && (before == device || hipSetDevice(device) == hipSuccess);
+    }
+    ~OnDevice() { if (ok && before != device) (void)hipSetDevice(before); }
+};
+#define ON_DEVICE() OnDevice on_(ctx->c); if (!on_.ok) return EVOMOE_EHIP
+
+evomoe_status check_topk(const evomoe_topk* o, int E) {
+    if (!o || (o->score != EVOMOE_SOFTMAX && o->score != EVOMOE_SIGMOID)) return EVOMOE_EINVAL;
+    if (o->groups < 1 || E % o->groups || o->top_groups < 1 || o->top_groups > o->groups) return EVOMOE_EINVAL;
+    if (o->group_keys != 1 && o->group_keys != 2) return EVOMOE_EINVAL;
+    if (o->k < 1 || o->k > o->top_groups * (E / o->groups)) return EVOMOE_EINVAL;
+    if (o->renormalise != 0 && o->renormalise != 1) return EVOMOE_EINVAL;
+    return o->scale > 0.f && o->scale < INFINITY ? EVOMOE_OK : EVOMOE_EINVAL;
+}
+
 #define REQUIRE_PTR(p) \
     do { if (!(p) || !aligned16(p)) return EVOMOE_EINVAL; } while (0)
 #define OPTIONAL_PTR(p) \
@@ -152,9 +181,10 @@ const char* evomoe_status_string(evomoe_status s) {
 
 size_t evomoe_workspace_bytes(const evomoe_shape* shape) {
     if (check_shape(shape) != EVOMOE_OK) return 0;
-    const size_t a = ffn_bwd_workspace_bytes(*shape), b = gate_bwd_workspace_bytes(*shape);
+    const size_t a = ffn_bwd_workspace_bytes(*shape), b = gate_bwd_workspace_bytes(*shape),
+                 n = rmsnorm_bwd_workspace_bytes(*shape);
     const size_t m = a > b ? a : b;
-    return (m + 255) & ~(size_t)255;
+    return ((m > n ? m : n) + 255) & ~(size_t)255;
 }
 
 evomoe_status evomoe_dts_gate(evomoe_ctx* ctx, const evomoe_shape* shape, const void* x,
@@ -391,6 +421,109 @@ evomoe_status evomoe_diversify(evomoe_ctx* ctx, const evomoe_shape* shape, const
     if ((int64_t)shape->d * shape->F >= ((int64_t)1 << 48)) return EVOMOE_EUNSUPPORTED;
     return from_hip(launch_diversify(ctx->c, *shape, W1_shared, b1_shared, W2_shared, b2_shared, seed, mask_ratio,
                                      W1, b1, W2, b2));
+}
+
+evomoe_status evomoe_gate_logits(evomoe_ctx* ctx, const evomoe_shape* shape, const void* x, const float* Wg,
+                                 const float* bg, float* logits) {
+    CHECK_CTX_SHAPE();
+    REQUIRE_PTR(x); REQUIRE_PTR(Wg); REQUIRE_PTR(logits); OPTIONAL_PTR(bg);
+    ON_DEVICE();
+    if (shape->dtype == EVOMOE_BF16) {
+        evomoe_status st = ensure_wg_planes(ctx->c, (size_t)3 * 64 * ((shape->d + 31) / 32 * 32) * sizeof(uint16_t));
+        if (st != EVOMOE_OK) return st;
+    }
+    return from_hip(launch_gate_logits(ctx->c, *shape, x, Wg, bg, logits));
+}
+
+evomoe_status evomoe_gate_logits_bwd(evomoe_ctx* ctx, const evomoe_shape* shape, const float* dlogits, const void* x,
+                                     const float* Wg, const void* dx_in, float* dWg, float* dbg, void* dx,
+                                     void* workspace, size_t workspace_bytes) {
+    CHECK_CTX_SHAPE();
+    REQUIRE_PTR(dlogits); REQUIRE_PTR(x); REQUIRE_PTR(Wg); REQUIRE_PTR(dWg); REQUIRE_PTR(dx);
+    OPTIONAL_PTR(dx_in); OPTIONAL_PTR(dbg);
+    if (!workspace || !aligned16(workspace) || workspace_bytes < gate_bwd_workspace_bytes(*shape))
+        return EVOMOE_EWORKSPACE;
+    ON_DEVICE();
+    return from_hip(launch_gate_logits_bwd(ctx->c, *shape, dlogits, x, Wg, dx_in, dWg, dbg, dx, (float*)workspace));
+}
+
+evomoe_status evomoe_topk_gate(evomoe_ctx* ctx, const evomoe_shape* shape, const evomoe_topk* topk, const float* logits,
+                               const float* balance_bias, float* scores, float* gate_w, uint64_t* mask_bits,
+                               int32_t* counts, int32_t* k_per_token, int32_t* block_hist) {
+    CHECK_CTX_SHAPE();
+    if (evomoe_status st = check_topk(topk, shape->E); st != EVOMOE_OK) return st;
+    REQUIRE_PTR(logits); REQUIRE_PTR(gate_w); REQUIRE_PTR(mask_bits); REQUIRE_PTR(counts);
+    OPTIONAL_PTR(balance_bias); OPTIONAL_PTR(scores); OPTIONAL_PTR(k_per_token); OPTIONAL_PTR(block_hist);
+    ON_DEVICE();
+    return from_hip(launch_topk_gate(ctx->c, *shape, *topk, logits, balance_bias, scores, gate_w, mask_bits, counts,
+                                     k_per_token, block_hist));
+}
+
+evomoe_status evomoe_topk_gate_bwd(evomoe_ctx* ctx, const evomoe_shape* shape, const evomoe_topk* topk,
+                                   const float* dG_pairs, const int32_t* tok_off, const int32_t* tok_rows,
+                                   const float* logits, const uint64_t* mask_bits, const float* dscore_coef,
+                                   float loss_scale, float* dlogits) {
+    CHECK_CTX_SHAPE();
+    if (evomoe_status st = check_topk(topk, shape->E); st != EVOMOE_OK) return st;
+    REQUIRE_PTR(dG_pairs); REQUIRE_PTR(tok_off); REQUIRE_PTR(tok_rows); REQUIRE_PTR(logits); REQUIRE_PTR(mask_bits);
+    REQUIRE_PTR(dlogits);
+    if (dscore_coef && (reinterpret_cast<uintptr_t>(dscore_coef) & 3u)) return EVOMOE_EINVAL;
+    ON_DEVICE();
+    return from_hip(launch_topk_gate_bwd(ctx->c, *shape, *topk, dG_pairs, tok_off, tok_rows, logits, mask_bits,
+                                         dscore_coef, loss_scale, dlogits));
+}
+
+evomoe_status evomoe_add_rmsnorm(evomoe_ctx* ctx, const evomoe_shape* shape, const void* x, const void* residual,
+                                 const float* gamma, float eps, void* h, void* y, float* rstd, void* q,
+                                 uint8_t* q_scale) {
+    CHECK_CTX_SHAPE();
+    REQUIRE_PTR(x); REQUIRE_PTR(gamma);
+    OPTIONAL_PTR(residual); OPTIONAL_PTR(h); OPTIONAL_PTR(y); OPTIONAL_PTR(rstd); OPTIONAL_PTR(q); OPTIONAL_PTR(q_scale);
+    if (!(eps > 0.f) || !(eps < INFINITY) || (!h && !y && !q) || (q != nullptr) != (q_scale != nullptr) || (h && h == y))
+        return EVOMOE_EINVAL;
+    if (q && shape->d % 32) return EVOMOE_EUNSUPPORTED;
+    ON_DEVICE();
+    return from_hip(launch_add_rmsnorm(ctx->c, *shape, x, residual, gamma, eps, h, y, rstd, q, q_scale));
+}
+
+evomoe_status evomoe_add_rmsnorm_bwd(evomoe_ctx* ctx, const evomoe_shape* shape, const void* dy, const void* dh,
+                                     const void* h, const float* gamma, const float* rstd, void* dx, float* dgamma,
+                                     void* workspace, size_t workspace_bytes) {
+    CHECK_CTX_SHAPE();
+    REQUIRE_PTR(dy); REQUIRE_PTR(h); REQUIRE_PTR(gamma); REQUIRE_PTR(rstd); REQUIRE_PTR(dx);
+    OPTIONAL_PTR(dh); OPTIONAL_PTR(dgamma);
+    if (dgamma && (!workspace || !aligned16(workspace) || workspace_bytes < rmsnorm_bwd_workspace_bytes(*shape)))
+        return EVOMOE_EWORKSPACE;
+    ON_DEVICE();
+    return from_hip(launch_add_rmsnorm_bwd(ctx->c, *shape, dy, dh, h, gamma, rstd, dx, dgamma, workspace));
+}
+
+evomoe_status evomoe_quantize_mx8(evomoe_ctx* ctx, int64_t rows, int64_t cols, int dtype, const void* src, void* q,
+                                  uint8_t* q_scale) {
+    if (!ctx || rows <= 0 || cols <= 0 || (dtype != EVOMOE_F32 && dtype != EVOMOE_BF16)) return EVOMOE_EINVAL;
+    if (cols % 32 || rows > ((int64_t)1 << 40) / cols) return EVOMOE_EUNSUPPORTED;
+    REQUIRE_PTR(src); REQUIRE_PTR(q); REQUIRE_PTR(q_scale);
+    ON_DEVICE();
+    return from_hip(launch_quantize_mx8(ctx->c, rows, cols, dtype, src, q, q_scale));
+}
+
+size_t evomoe_workspace_bytes_mx8(const evomoe_shape* shape) {
+    return check_mx8_shape(shape) == EVOMOE_OK ? ffn_mx8_workspace_bytes(*shape) : 0;
+}
+
+evomoe_status evomoe_expert_ffn_mx8(evomoe_ctx* ctx, const evomoe_shape* shape, const void* x_q, const uint8_t* x_scale,
+                                    const int32_t* pair_token, const int32_t* expert_offsets, const void* W1_q,
+                                    const uint8_t* W1_scale, const float* b1, const void* W2_q, const uint8_t* W2_scale,
+                                    const float* b2, void* O, void* workspace, size_t workspace_bytes) {
+    if (!ctx) return EVOMOE_EINVAL;
+    if (evomoe_status st = check_mx8_shape(shape); st != EVOMOE_OK) return st;
+    REQUIRE_PTR(x_q); REQUIRE_PTR(x_scale); REQUIRE_PTR(expert_offsets); REQUIRE_PTR(W1_q); REQUIRE_PTR(W1_scale);
+    REQUIRE_PTR(W2_q); REQUIRE_PTR(W2_scale); REQUIRE_PTR(O);
+    OPTIONAL_PTR(pair_token); OPTIONAL_PTR(b1); OPTIONAL_PTR(b2);
+    if (!workspace || !aligned16(workspace) || workspace_bytes < ffn_mx8_workspace_bytes(*shape)) return EVOMOE_EWORKSPACE;
+    ON_DEVICE();
+    return from_hip(launch_expert_ffn_mx8(ctx->c, *shape, x_q, x_scale, pair_token, expert_offsets, W1_q, W1_scale, b1,
+                                          W2_q, W2_scale, b2, O, workspace));
 }
 
 evomoe_status evomoe_hint_pairs(evomoe_ctx* ctx, int64_t expected_pairs) {

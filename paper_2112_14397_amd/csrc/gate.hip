@@ -1,4 +1,4 @@
-// DTS gate, forward and backward (EvoMoE Stage 2: Eq. gumbel_softmax, Eq. adaptive_sparsity, Algorithm 2).
+// DTS gate, forward and backward, and the gate's logits and their gradients alone (EvoMoE Stage 2: Eq. gumbel_softmax, Eq. adaptive_sparsity, Algorithm 2).
 //
 // Forward: logits on the matrix cores with float32-exact products (f32 MFMA for a float32 layer, three
 // bf16 MFMAs against a hi/mid/lo split of W_g for a bf16 layer: a selection decided by g' > c must not
@@ -16,6 +16,46 @@ namespace evomoe {
 // ---------------------------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------------------------
+// Adds the four waves' partial tiles in wave order (fixed order => reproducible bits) into zsum [16 RT][16 NE + 4] (LDS).
+template <int NE, int RT>
+__device__ __forceinline__ void add_waves(f32x4 (&acc)[RT][NE], float* zsum, int wave, int q, int i16) {
+    constexpr int LDZ = 16 * NE + 4;
+    for (int w = 0; w < 4; ++w) {
+        if (wave == w) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int n = 0; n < NE; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int idx = (rt * 16 + 4 * q + r) * LDZ + n * 16 + i16;
+                        const float v = acc[rt][n][r];
+                        zsum[idx] = (w == 0) ? v : zsum[idx] + v;
+                    }
+        }
+        __syncthreads();
+    }
+}
+
+// Tail of the kernels that only want the logits (evomoe_gate_logits): sums + bias, written out.
+template <int NE, int RT, int SUB>
+__device__ __forceinline__ void logits_finish(f32x4 (&acc)[RT][NE], const float* __restrict__ bg, int T, int E,
+                                              float* __restrict__ logits)
+{
+    constexpr int TPB = 16 * RT, LDZ = 16 * NE + 4;
+    __shared__ float zsum_all[SUB * TPB * LDZ];
+    const int tid = threadIdx.x & 255, lane = tid & 63, wave = tid >> 6;
+    const int sub_blk = SUB > 1 ? threadIdx.x >> 8 : 0;
+    const int t0 = (blockIdx.x * SUB + sub_blk) * TPB;
+    float* zsum = zsum_all + sub_blk * TPB * LDZ;
+    add_waves<NE, RT>(acc, zsum, wave, lane >> 4, lane & 15);
+    const int n = min(TPB, T - t0) * E;                       // (below zero for a sub-block without tokens)
+    for (int i = tid; i < n; i += 256) {
+        const int tl = i / E, e = i - tl * E;
+        logits[(size_t)t0 * E + i] = zsum[tl * LDZ + e] + (bg ? bg[e] : 0.f);
+    }
+}
+
 // Common tail of the gate kernels.  In: per-wave partial logit tiles acc[rt][n] (MFMA 16x16 layout:
 // element r of lane (q = lane/16, i16 = lane%16) is token row 4q+r, expert column 16n+i16).
 // Adds the four waves' tiles in wave order (fixed order => reproducible bits), then 16/RT threads per
@@ -44,22 +84,7 @@ __device__ __forceinline__ void gate_finish(
     float* zsum = zsum_all + sub_blk * TPB * LDZ;
 
     if (threadIdx.x < 64) cnt[threadIdx.x] = 0;
-    // add the four waves' partial tiles in wave order (fixed order => reproducible bits)
-    for (int w = 0; w < 4; ++w) {
-        if (wave == w) {
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                for (int n = 0; n < NE; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int idx = (rt * 16 + 4 * q + r) * LDZ + n * 16 + i16;
-                        const float v = acc[rt][n][r];
-                        zsum[idx] = (w == 0) ? v : zsum[idx] + v;
-                    }
-        }
-        __syncthreads();
-    }
+    add_waves<NE, RT>(acc, zsum, wave, q, i16);
 
     // ---- softmax / threshold: TPT threads per token ----
     const int tl = tid / TPT, sub = tid % TPT;
@@ -147,7 +172,8 @@ __device__ __forceinline__ void gate_finish(
 
 // float32 layer: logits with v_mfma_f32_16x16x4_f32 (exact float32 products).  Block = 4 waves; the
 // block owns 16*RT consecutive tokens; each wave takes every 4th K-slab of all of them.
-template <typename TX, int NE, int RT, int SUB = 1>
+// LOGITS: gprime takes the logits, and nothing else is written.
+template <typename TX, int NE, int RT, int SUB = 1, bool LOGITS = false>
 __global__ __launch_bounds__(256 * SUB) void dts_gate_kernel(
     const TX* __restrict__ x, const float* __restrict__ Wg, const float* __restrict__ bg,
     const float* __restrict__ noise, float tau, float c, int T, int d, int E,
@@ -193,7 +219,8 @@ __global__ __launch_bounds__(256 * SUB) void dts_gate_kernel(
             }
         }
     }
-    gate_finish<NE, RT, SUB>(acc, bg, noise, tau, c, T, E, gprime, gate_w, mask_bits, k_per_token, counts, block_hist);
+    if constexpr (LOGITS) logits_finish<NE, RT, SUB>(acc, bg, T, E, gprime);
+    else gate_finish<NE, RT, SUB>(acc, bg, noise, tau, c, T, E, gprime, gate_w, mask_bits, k_per_token, counts, block_hist);
 }
 
 // bf16 layer.  x is exact in bf16, so W_g is split into three bf16 terms (hi + mid + lo carry all 24
@@ -205,13 +232,13 @@ __global__ __launch_bounds__(256 * SUB) void dts_gate_kernel(
 // a k-block (E = 64) are 12 KB in a row: full cache lines, spread evenly over the L2 channels (rows of a plain
 // transposed copy are 2 d bytes apart, and every block of the grid asks for the same sixteen of them at the
 // same time).  Zero beyond E and beyond d.  The kernel also clears the integer sums the gate adds to
-// (planes == null, float32 layer: clears only).
+// (planes == null, float32 layer: clears only; counts == null, logits alone: splits only).
 __global__ __launch_bounds__(256) void gate_prep_kernel(const float* __restrict__ Wg, int d, int E, int NE,
                                                         uint16_t* __restrict__ planes, int32_t* __restrict__ counts,
                                                         int32_t* __restrict__ block_hist, int n_hist)
 {
     const int i = blockIdx.x * 256 + threadIdx.x;          // over nkb * NE * 512 elements of one term, destination order
-    if (i < E) counts[i] = 0;
+    if (counts && i < E) counts[i] = 0;
     if (block_hist && i < n_hist) block_hist[i] = 0;
     const int nkb = (d + 31) / 32;
     if (!planes || i >= nkb * NE * 512) return;
@@ -232,7 +259,7 @@ __global__ __launch_bounds__(256) void gate_prep_kernel(const float* __restrict_
 
 // SUB > 1 (one block, at most 16 experts): there is no split copy; every wave reads the float32 weights of its k-blocks
 // together with x and splits them itself, into the same three terms.
-template <int NE, int RT, int SUB = 1>
+template <int NE, int RT, int SUB = 1, bool LOGITS = false>
 __global__ __launch_bounds__(256 * SUB) void dts_gate_bf16_kernel(
     const bf16_t* __restrict__ x, const bf16_t* __restrict__ planes, const float* __restrict__ Wg,
     const float* __restrict__ bg,
@@ -320,7 +347,15 @@ __global__ __launch_bounds__(256 * SUB) void dts_gate_bf16_kernel(
                 }
         }
     }
-    gate_finish<NE, RT, SUB>(acc, bg, noise, tau, c, T, E, gprime, gate_w, mask_bits, k_per_token, counts, block_hist);
+    if constexpr (LOGITS) logits_finish<NE, RT, SUB>(acc, bg, T, E, gprime);
+    else gate_finish<NE, RT, SUB>(acc, bg, noise, tau, c, T, E, gprime, gate_w, mask_bits, k_per_token, counts, block_hist);
+}
+
+hipError_t launch_clear_counts(const Ctx& c, const evomoe_shape& s, int32_t* counts, int32_t* block_hist) {
+    const int n_hist = dispatch_blocks(s) * s.E, n = n_hist > s.E ? n_hist : s.E;
+    hipLaunchKernelGGL(gate_prep_kernel, dim3((n + 255) / 256), dim3(256), 0, c.stream, (const float*)nullptr, s.d, s.E, 0,
+                       (uint16_t*)nullptr, counts, block_hist, n_hist);
+    return hipGetLastError();
 }
 
 static int pick_rt(const Ctx& c, const evomoe_shape& s) {
@@ -425,6 +460,48 @@ hipError_t launch_dts_gate(const Ctx& c, const evomoe_shape& s, const void* x, c
                                  counts, k_per_token, block_hist);
 }
 
+template <typename TX, int NE, int RT>
+static hipError_t logits_launch_t(const Ctx& c, const evomoe_shape& s, const void* x, const float* Wg, const float* bg,
+                                  float* logits) {
+    const int blocks = (s.T + 16 * RT - 1) / (16 * RT);
+    ProfScope ps(c, EVOMOE_K_GATE_LOGITS);
+    if constexpr (std::is_same<TX, bf16_t>::value) {
+        const int n = (s.d + 31) / 32 * NE * 512;
+        hipLaunchKernelGGL(gate_prep_kernel, dim3((n + 255) / 256), dim3(256), 0, c.stream, Wg, s.d, s.E, NE,
+                           c.wg_planes, (int32_t*)nullptr, (int32_t*)nullptr, 0);
+        hipLaunchKernelGGL((dts_gate_bf16_kernel<NE, RT, 1, true>), dim3(blocks), dim3(256), 0, c.stream, (const bf16_t*)x,
+                           (const bf16_t*)c.wg_planes, Wg, bg, (const float*)nullptr, 1.f, 0.f, s.T, s.d, s.E, logits,
+                           (float*)nullptr, (uint64_t*)nullptr, (int32_t*)nullptr, (int32_t*)nullptr, (int32_t*)nullptr);
+    } else {
+        hipLaunchKernelGGL((dts_gate_kernel<TX, NE, RT, 1, true>), dim3(blocks), dim3(256), 0, c.stream, (const TX*)x, Wg, bg,
+                           (const float*)nullptr, 1.f, 0.f, s.T, s.d, s.E, logits, (float*)nullptr, (uint64_t*)nullptr,
+                           (int32_t*)nullptr, (int32_t*)nullptr, (int32_t*)nullptr);
+    }
+    return hipGetLastError();
+}
+template <typename TX>
+static hipError_t logits_launch(const Ctx& c, const evomoe_shape& s, const void* x, const float* Wg, const float* bg,
+                                float* logits) {
+    const int rt = pick_rt(c, s);
+    auto with = [&](auto ne) {
+        constexpr int NE = decltype(ne)::value;
+        return rt == 4 ? logits_launch_t<TX, NE, 4>(c, s, x, Wg, bg, logits)
+             : rt == 2 ? logits_launch_t<TX, NE, 2>(c, s, x, Wg, bg, logits)
+                       : logits_launch_t<TX, NE, 1>(c, s, x, Wg, bg, logits);
+    };
+    switch ((s.E + 15) / 16) {
+        case 1: return with(std::integral_constant<int, 1>{});
+        case 2: return with(std::integral_constant<int, 2>{});
+        case 3: return with(std::integral_constant<int, 3>{});
+        default: return with(std::integral_constant<int, 4>{});
+    }
+}
+hipError_t launch_gate_logits(const Ctx& c, const evomoe_shape& s, const void* x, const float* Wg, const float* bg,
+                              float* logits) {
+    return s.dtype == EVOMOE_BF16 ? logits_launch<bf16_t>(c, s, x, Wg, bg, logits)
+                                  : logits_launch<float>(c, s, x, Wg, bg, logits);
+}
+
 // ---------------------------------------------------------------------------------------------
 // backward
 // ---------------------------------------------------------------------------------------------
@@ -476,11 +553,11 @@ template <int CPT> struct RowVec<float, CPT> {
 };
 // float32 layer.  One block = TC tokens x 256*CPT columns of x.  A thread owns CPT consecutive columns k: it keeps W_g[k,:]
 // and a partial dWg[k,:] in registers and walks the chunk's tokens:
-//   dx[s,k] += <dz[s,:], W_g[k,:]>,   dWg_part[k,:] += x[s,k] dz[s,:].
+//   dx[s,k] = dx_in[s,k] + <dz[s,:], W_g[k,:]>,   dWg_part[k,:] += x[s,k] dz[s,:]     (dx_in may be dx, or null = 0).
 template <typename TX, int EP, int CPT>
 __global__ __launch_bounds__(256) void gate_bwd_kernel(
     const float* __restrict__ dz, const TX* __restrict__ x, const float* __restrict__ Wg,
-    int T, int d, int E, int TC, TX* __restrict__ dx, float* __restrict__ dWg_part,
+    int T, int d, int E, int TC, const TX* dx_in, TX* dx, float* __restrict__ dWg_part,
     float* __restrict__ dbg_part)
 {
     extern __shared__ float sdz[];          // [TC][EP], zero beyond E
@@ -517,7 +594,10 @@ __global__ __launch_bounds__(256) void gate_bwd_kernel(
             const int s = min(sb + u, ns - 1);
             const size_t off = (size_t)(s0 + s) * d + k;
             RowVec<TX, CPT>::load(x + off, xv[buf][u]);
-            RowVec<TX, CPT>::load(dx + off, dxv[buf][u]);
+            if (dx_in) RowVec<TX, CPT>::load(dx_in + off, dxv[buf][u]);
+            else
+#pragma unroll
+                for (int c = 0; c < CPT; ++c) dxv[buf][u][c] = 0.f;
         }
     };
     auto use_group = [&](int sb, int buf) {
@@ -561,7 +641,7 @@ __global__ __launch_bounds__(256) void gate_bwd_kernel(
 }
 
 // ---- bf16 layer: both contractions of the gate backward on the matrix cores ------------------------------
-//   dx[s,k]   += sum_e dz[s,e] W_g[k,e]      (M = tokens, N = columns of x, K = experts)
+//   dx[s,k]    = dx_in[s,k] + sum_e dz[s,e] W_g[k,e]      (M = tokens, N = columns of x, K = experts)
 //   dWg[k,e]   = sum_s x[s,k] dz[s,e]        (M = columns of x, N = experts, K = tokens)
 // with v_mfma_f32_32x32x16_bf16.  x is bf16 already; the float32 factors are split into bf16 terms so that the
 // products stay (nearly) exact: dz = hi + mid + lo (all 24 mantissa bits; x dz is then exact, accumulated in
@@ -602,7 +682,7 @@ __device__ __forceinline__ bf16x8 lds_read_tr(const unsigned char* q, int row_by
 template <int KE, int NE>
 __global__ __launch_bounds__(256, 2) void gate_bwd_mfma_kernel(
     const float* __restrict__ dz, const bf16_t* __restrict__ x, const float* __restrict__ Wg, int T, int d, int E,
-    int tokens_per_block, bf16_t* __restrict__ dx, float* __restrict__ dWg_part, float* __restrict__ dbg_part)
+    int tokens_per_block, const bf16_t* dx_in, bf16_t* dx, float* __restrict__ dWg_part, float* __restrict__ dbg_part)
 {
     constexpr int EPL = 32 * NE;                     // experts per LDS row (zero beyond E)
     constexpr int DZN = kGbTok * EPL / 256;          // dz values per thread and chunk
@@ -666,7 +746,7 @@ __global__ __launch_bounds__(256, 2) void gate_bwd_mfma_kernel(
 #pragma unroll
         for (int it = 0; it < 4; ++it) {
             const int t = min(s0 + it * 8 + trow, T - 1);
-            dxr[it] = *reinterpret_cast<const u32x4*>(dx + (size_t)t * d + gcol);
+            dxr[it] = dx_in ? *reinterpret_cast<const u32x4*>(dx_in + (size_t)t * d + gcol) : u32x4{0u, 0u, 0u, 0u};
         }
     };
     if (nch > 0) {
@@ -829,7 +909,7 @@ size_t gate_bwd_workspace_bytes(const evomoe_shape& s) {
 
 template <typename TX>
 static hipError_t gate_bwd_t(const Ctx& c, const evomoe_shape& s, const float* dz, const void* x,
-                             const float* Wg, void* dx, float* dWg_part, float* dbg_part, int tc,
+                             const float* Wg, const void* dx_in, void* dx, float* dWg_part, float* dbg_part, int tc,
                              int nchunk) {
     const int ep = ((s.E + 15) / 16) * 16;
     // Columns per thread: as many as the registers hold (2*CPT*EP), but no more than leave every thread of a block some:
@@ -841,7 +921,7 @@ static hipError_t gate_bwd_t(const Ctx& c, const evomoe_shape& s, const float* d
     const size_t lds = (size_t)tc * ep * sizeof(float);
 #define EVOMOE_GB(EPV, CPTV)                                                                     \
     hipLaunchKernelGGL((gate_bwd_kernel<TX, EPV, CPTV>), grid, dim3(256), lds, c.stream, dz,     \
-                       (const TX*)x, Wg, s.T, s.d, s.E, tc, (TX*)dx, dWg_part, dbg_part)
+                       (const TX*)x, Wg, s.T, s.d, s.E, tc, (const TX*)dx_in, (TX*)dx, dWg_part, dbg_part)
     if (ep == 16 && cpt == 4) EVOMOE_GB(16, 4);
     else if (ep == 16 && cpt == 2) EVOMOE_GB(16, 2);
     else if (ep == 16) EVOMOE_GB(16, 1);
@@ -853,18 +933,46 @@ static hipError_t gate_bwd_t(const Ctx& c, const evomoe_shape& s, const float* d
     return hipGetLastError();
 }
 
+// part: chunk c's partial sums, [dWg partial: d x E][dbg partial: E], contiguous
+hipError_t launch_gate_logits_bwd(const Ctx& c, const evomoe_shape& s, const float* dz, const void* x, const float* Wg,
+                                  const void* dx_in, float* dWg, float* dbg, void* dx, float* part) {
+    const int tc = gate_bwd_chunk_tokens(s);
+    const bool mfma = gate_bwd_use_mfma(s);
+    const GbPlan plan = gate_bwd_mfma_plan(s);
+    const int nchunk = mfma ? plan.nblk : (s.T + tc - 1) / tc;
+    float* dbg_part = part + (size_t)s.d * s.E;
+    hipError_t err;
+    {
+        ProfScope ps(c, EVOMOE_K_GATE_BWD_MAIN);
+        if (mfma) {
+            const dim3 grid(plan.nblk, plan.slices);
+#define EVOMOE_GBM(KEV, NEV)                                                                             \
+    hipLaunchKernelGGL((gate_bwd_mfma_kernel<KEV, NEV>), grid, dim3(256), 0, c.stream, dz, (const bf16_t*)x, Wg, \
+                       s.T, s.d, s.E, plan.tokens_per_block, (const bf16_t*)dx_in, (bf16_t*)dx, part, dbg_part)
+            if (s.E <= 16) EVOMOE_GBM(1, 1);
+            else if (s.E <= 32) EVOMOE_GBM(2, 1);
+            else if (s.E <= 48) EVOMOE_GBM(3, 2);
+            else EVOMOE_GBM(4, 2);
+#undef EVOMOE_GBM
+            err = hipGetLastError();
+        } else {
+            err = gate_bwd_t<float>(c, s, dz, x, Wg, dx_in, dx, part, dbg_part, tc, nchunk);
+        }
+    }
+    if (err != hipSuccess) return err;
+    const size_t n0 = (size_t)s.d * s.E, n1 = (size_t)s.E;
+    ProfScope ps(c, EVOMOE_K_GATE_BWD_REDUCE);
+    hipLaunchKernelGGL(sum_chunks_kernel, dim3((n0 + n1 + 63) / 64), dim3(256), 0, c.stream, part, nchunk, n0,
+                       n1, dWg, dbg);
+    return hipGetLastError();
+}
+
 hipError_t launch_dts_gate_bwd(const Ctx& c, const evomoe_shape& s, const float* dG_pairs,
                                const int32_t* tok_off, const int32_t* tok_rows, const float* gprime,
                                const uint64_t* mask_bits, float tau, const void* x, const float* Wg,
                                float* dWg, float* dbg, void* dx, void* workspace,
                                const float* dgprime_coef, float coef_scale) {
-    const int tc = gate_bwd_chunk_tokens(s);
-    const bool mfma = gate_bwd_use_mfma(s);
-    const GbPlan plan = gate_bwd_mfma_plan(s);
-    const int nchunk = mfma ? plan.nblk : (s.T + tc - 1) / tc;
     float* dz = (float*)workspace;
-    float* dWg_part = dz + (size_t)s.T * s.E;
-    float* dbg_part = dWg_part + (size_t)s.d * s.E;     // chunk c: [dWg partial: d x E][dbg partial: E], contiguous
     {
         ProfScope ps(c, EVOMOE_K_GATE_BWD_DZ);
 #define EVOMOE_DZ(EPV)                                                                                   \
@@ -880,28 +988,13 @@ hipError_t launch_dts_gate_bwd(const Ctx& c, const evomoe_shape& s, const float*
     }
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    {
-        ProfScope ps(c, EVOMOE_K_GATE_BWD_MAIN);
-        if (mfma) {
-            const dim3 grid(plan.nblk, plan.slices);
-#define EVOMOE_GBM(KEV, NEV)                                                                             \
-    hipLaunchKernelGGL((gate_bwd_mfma_kernel<KEV, NEV>), grid, dim3(256), 0, c.stream, dz, (const bf16_t*)x, Wg, \
-                       s.T, s.d, s.E, plan.tokens_per_block, (bf16_t*)dx, dWg_part, dbg_part)
-            if (s.E <= 16) EVOMOE_GBM(1, 1);
-            else if (s.E <= 32) EVOMOE_GBM(2, 1);
-            else if (s.E <= 48) EVOMOE_GBM(3, 2);
-            else EVOMOE_GBM(4, 2);
-#undef EVOMOE_GBM
-            err = hipGetLastError();
-        } else {
-            err = gate_bwd_t<float>(c, s, dz, x, Wg, dx, dWg_part, dbg_part, tc, nchunk);
-        }
-    }
-    if (err != hipSuccess) return err;
-    const size_t n0 = (size_t)s.d * s.E, n1 = (size_t)s.E;
-    ProfScope ps(c, EVOMOE_K_GATE_BWD_REDUCE);
-    hipLaunchKernelGGL(sum_chunks_kernel, dim3((n0 + n1 + 63) / 64), dim3(256), 0, c.stream, dWg_part, nchunk, n0,
-                       n1, dWg, dbg);
+    return launch_gate_logits_bwd(c, s, dz, x, Wg, dx, dWg, dbg, dx, dz + (size_t)s.T * s.E);
+}
+
+// out[i] = sum of rows of part [n_rows][n], i < n
+hipError_t launch_sum_rows(const Ctx& c, const float* part, int n_rows, size_t n, float* out) {
+    hipLaunchKernelGGL(sum_chunks_kernel, dim3((n + 63) / 64), dim3(256), 0, c.stream, part, n_rows, n, (size_t)0, out,
+                       (float*)nullptr);
     return hipGetLastError();
 }
 

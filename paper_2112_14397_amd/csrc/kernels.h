@@ -15,10 +15,42 @@ hipError_t launch_dts_gate_bwd(const Ctx& c, const evomoe_shape& s, const float*
                                float* dWg, float* dbg, void* dx, void* workspace,
                                const float* dgprime_coef = nullptr, float coef_scale = 0.f);
 size_t gate_bwd_workspace_bytes(const evomoe_shape& s);
+hipError_t launch_gate_logits(const Ctx& c, const evomoe_shape& s, const void* x, const float* Wg, const float* bg,
+                              float* logits);
+// part: gate_bwd_workspace_bytes(s) hold it
+hipError_t launch_gate_logits_bwd(const Ctx& c, const evomoe_shape& s, const float* dz, const void* x, const float* Wg,
+                                  const void* dx_in, float* dWg, float* dbg, void* dx, float* part);
+// clears counts [E] and block_hist (may be null)
+hipError_t launch_clear_counts(const Ctx& c, const evomoe_shape& s, int32_t* counts, int32_t* block_hist);
+hipError_t launch_sum_rows(const Ctx& c, const float* part, int n_rows, size_t n, float* out);
 // balance loss: scratch holds balance_blocks(s) * E floats of per-block column sums of g'
 int balance_blocks(const evomoe_shape& s);
 hipError_t launch_balance_loss(const Ctx& c, const evomoe_shape& s, const float* gprime, const int32_t* counts,
                                float alpha, float* loss, float* dgprime_coef);
+
+// topk.hip
+hipError_t launch_topk_gate(const Ctx& c, const evomoe_shape& s, const evomoe_topk& o, const float* logits,
+                            const float* balance_bias, float* scores, float* gate_w, uint64_t* mask_bits,
+                            int32_t* counts, int32_t* k_per_token, int32_t* block_hist);
+hipError_t launch_topk_gate_bwd(const Ctx& c, const evomoe_shape& s, const evomoe_topk& o, const float* dG_pairs,
+                                const int32_t* tok_off, const int32_t* tok_rows, const float* logits,
+                                const uint64_t* mask_bits, const float* dscore_coef, float loss_scale, float* dlogits);
+
+// norm.hip
+hipError_t launch_add_rmsnorm(const Ctx& c, const evomoe_shape& s, const void* x, const void* residual,
+                              const float* gamma, float eps, void* h, void* y, float* rstd, void* q, uint8_t* q_scale);
+hipError_t launch_add_rmsnorm_bwd(const Ctx& c, const evomoe_shape& s, const void* dy, const void* dh, const void* h,
+                                  const float* gamma, const float* rstd, void* dx, float* dgamma, void* workspace);
+size_t rmsnorm_bwd_workspace_bytes(const evomoe_shape& s);
+hipError_t launch_quantize_mx8(const Ctx& c, int64_t rows, int64_t cols, int dtype, const void* src, void* q,
+                               uint8_t* q_scale);
+
+// ffn_mx8.hip
+size_t ffn_mx8_workspace_bytes(const evomoe_shape& s);
+hipError_t launch_expert_ffn_mx8(const Ctx& c, const evomoe_shape& s, const void* x_q, const uint8_t* x_scale,
+                                 const int32_t* pair_token, const int32_t* expert_offsets, const void* W1_q,
+                                 const uint8_t* W1_scale, const float* b1, const void* W2_q, const uint8_t* W2_scale,
+                                 const float* b2, void* O, void* workspace);
 
 // dispatch.hip
 hipError_t launch_dispatch(const Ctx& c, const evomoe_shape& s, const uint64_t* mask_bits,
