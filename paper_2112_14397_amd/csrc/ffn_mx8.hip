@@ -8,6 +8,7 @@
 #include <type_traits>
 
 #include "kernels.h"
+#include "mfma_tools.h"
 #include "mx8.h"
 
 namespace evomoe {
@@ -103,10 +104,283 @@ __global__ __launch_bounds__(64) void mx8_gemm_kernel(Mx8Args p)
     }
 }
 
-template <bool FIRST> hipError_t launch(const Ctx& c, const evomoe_shape& s, const Mx8Args& a) {
+// gelu(h) = max(h, 0) - x 2^p(x), x = |h|: 2^p is Phi(-x), p of degree five fitted for the least largest error of the product,
+// 5e-7 with float32's own, for every finite h (p falls to -inf).  Ten VALU instructions and an exponential.
+__device__ __forceinline__ float gelu5(float h) {
+    const float x = fabsf(h);
+    float p = -0.000473309294f;
+    p = fmaf(p, x, 0.00708455719f);
+    p = fmaf(p, x, -0.0518273829f);
+    p = fmaf(p, x, -0.459992439f);
+    p = fmaf(p, x, -1.15078785f);
+    p = fmaf(p, x, -1.00003762f);
+    return fmaf(-x, __builtin_amdgcn_exp2f(p), relu(h));
+}
+
+// v_mfma_scale_f32_32x32x64_f8f6f4: lane (h = lane / 32, i = lane % 32) brings the k's 16 h .. 16 h + 15 and 32 + 16 h .. of row i of
+// either operand, and the scale of that row's k's 32 h .. 32 h + 31 in byte `OP` of sa, sb; it receives, of column i, the rows
+// 8 (r / 4) + 4 h + r % 4, r = 0 .. 15.
+template <int OP> __device__ __forceinline__ f32x16 mfma32(i32x8 a, i32x8 b, f32x16 c, int sa, int sb) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, OP, sa, OP, sb);
+}
+
+// Exchanges the upper half of a with the lower half of b.
+__device__ __forceinline__ void swap_halves(uint32_t& a, uint32_t& b) {
+    const auto v = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    a = v[0];
+    b = v[1];
+}
+
+// The tile kernel, for contractions that are a multiple of 128.  A block of WX x WW waves computes BX rows of X by BW rows of W, a
+// wave TX x TW matrix instructions of 32 x 32.  The contraction runs in slabs of 128 bytes (one line of every row), two LDS stages
+// deep; a stage holds both operands' slabs, rows of 128 bytes with the 16-byte chunk c of row r at chunk c ^ (r >> 1 & 7), so that
+// sixteen lanes' reads of one chunk column meet all banks, and the four scale bytes of every row.  Loads go straight to the LDS.
+// Slab s + 2 is fetched into slab s's stage as soon as its last fragments are in registers, and lands while one and a half
+// slabs multiply.  Blocks are persistent and walk the tiles as the bf16 kernels do: expert by expert, column group by column
+// group, row tile by row tile, every XCD on a run of its own.
+template <bool FIRST, int BX, int BW, int WX, int WW, int WPE>
+__global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, int col_group)
+{
+    constexpr int NW = WX * WW, TX = BX / WX / 32, TW = BW / WW / 32;
+    constexpr int XLD = BX / 8 / NW, WLD = BW / 8 / NW;         // 1 KB load instructions per wave and slab
+    constexpr int ROWS = BX + BW, SLD = ROWS / 64 / NW;         // scale load instructions per wave and slab (64 rows each)
+    constexpr int STAGE = ROWS * 132;
+    static_assert(XLD * 8 * NW == BX && WLD * 8 * NW == BW && SLD * 64 * NW == ROWS && BX % 64 == 0, "whole instructions");
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ int offs[65], tstart[65];
+
+    const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wx = wave / WW, ww = wave % WW;
+    if (wave == 0) {          // lane e: expert e's rows, and the row tiles before it
+        const int begin = clamp_pairs(p.expert_offsets[min(lane, p.E)], p.P_cap),
+                  end = clamp_pairs(p.expert_offsets[min(lane + 1, p.E)], p.P_cap);
+        if (lane == 0) offs[0] = begin;
+        offs[lane + 1] = end;
+        int upto = (end - begin + BX - 1) / BX;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(upto, o, 64);
+            if (lane >= o) upto += v;
+        }
+        if (lane == 0) tstart[0] = 0;
+        tstart[lane + 1] = upto;
+    }
+    __syncthreads();
+    const int nct = (p.N + BW - 1) / BW, total = tstart[p.E] * nct, nslab = p.K / 128, kg = p.K / kMxGroup;
+    const bool xcds = (gridDim.x & 7) == 0;
+    int seq, seq_end, step;
+    if (xcds && col_group < nct) {
+        const int x = blockIdx.x & 7;
+        seq = (int)((int64_t)total * x / 8) + (blockIdx.x >> 3);
+        seq_end = (int)((int64_t)total * (x + 1) / 8);
+        step = gridDim.x >> 3;
+    } else {
+        seq = xcds ? (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3) : blockIdx.x;
+        seq_end = total;
+        step = gridDim.x;
+    }
+
+    for (; seq < seq_end; seq += step) {
+        // ---- where the tile lies ----
+        int g, row0, rows, n0;
+        {
+            const int first = tstart[lane], next = tstart[lane + 1], begin = offs[lane], end = offs[lane + 1];
+            g = __popcll(__ballot(seq >= next * nct));
+            const int t0 = __builtin_amdgcn_readlane(first, g), nrt = __builtin_amdgcn_readlane(next, g) - t0;
+            const int r = seq - t0 * nct, cg = r / (nrt * col_group), r2 = r - cg * nrt * col_group;
+            const int gc = min(col_group, nct - cg * col_group), rt = r2 / gc;
+            n0 = (cg * col_group + (r2 - rt * gc)) * BW;
+            row0 = __builtin_amdgcn_readlane(begin, g) + rt * BX;
+            rows = min(BX, __builtin_amdgcn_readlane(end, g) - row0);
+        }
+        g = __builtin_amdgcn_readfirstlane(g);
+        n0 = __builtin_amdgcn_readfirstlane(n0);
+        row0 = __builtin_amdgcn_readfirstlane(row0);
+        rows = __builtin_amdgcn_readfirstlane(rows);
+
+        // ---- addresses: rows beyond the tile repeat its last one, their products are not stored ----
+        const unsigned char* xb = p.X + (p.rows ? (int64_t)0 : (int64_t)row0 * p.K);
+        const unsigned char* xsb = p.Xs + (p.rows ? (int64_t)0 : (int64_t)row0 * kg);
+        const unsigned char* wb = p.W + ((int64_t)g * p.N + n0) * p.K;
+        const unsigned char* wsb = p.Ws + ((int64_t)g * p.N + n0) * kg;
+        uint32_t xo[XLD], wo[WLD], so[SLD];
+        const int lr = lane >> 3;                              // this lane's row of the eight that an instruction brings
+        auto x_row = [&](int r) { const int c = min(r, rows - 1); return p.rows ? (uint32_t)p.rows[row0 + c] : (uint32_t)c; };
+#pragma unroll
+        for (int i = 0; i < XLD; ++i) {
+            const int r = (wave + NW * i) * 8 + lr;
+            xo[i] = x_row(r) * (uint32_t)p.K + (((lane & 7) ^ (r >> 1 & 7)) << 4);
+        }
+#pragma unroll
+        for (int i = 0; i < WLD; ++i) {
+            const int r = (wave + NW * i) * 8 + lr;
+            wo[i] = (uint32_t)min(r, p.N - 1 - n0) * (uint32_t)p.K + (((lane & 7) ^ (r >> 1 & 7)) << 4);
+        }
+#pragma unroll
+        for (int i = 0; i < SLD; ++i) {
+            const int r = (wave + NW * i) * 64 + lane;        // X's rows, then W's
+            so[i] = (r < BX ? x_row(r) : (uint32_t)min(r - BX, p.N - 1 - n0)) * (uint32_t)kg;
+        }
+        // (what the compiler itself has loaded so far is complete, and known to be, before the loads that it does not count begin)
+        __builtin_amdgcn_s_waitcnt(0x0f70);                   // vmcnt(0)
+        block_sync_lds();                                     // the previous tile's readers are done with both stages
+        auto issue = [&](int slab) {
+            unsigned char* st = smem + (slab & 1) * STAGE;
+#pragma unroll
+            for (int i = 0; i < XLD; ++i) load_to_lds(xb, xo[i] + slab * 128, st + (wave + NW * i) * 1024);
+#pragma unroll
+            for (int i = 0; i < WLD; ++i) load_to_lds(wb, wo[i] + slab * 128, st + BX * 128 + (wave + NW * i) * 1024);
+#pragma unroll
+            for (int i = 0; i < SLD; ++i) {
+                const int r = (wave + NW * i) * 64;           // (64 rows of one operand: BX is a multiple of 64)
+                load_dword_to_lds(reinterpret_cast<const int32_t*>(r < BX ? xsb : wsb), so[i] + slab * 4,
+                                  reinterpret_cast<const int*>(st + ROWS * 128 + r * 4));
+            }
+        };
+        auto read = [&](int slab, int ks, i32x8 (&fw)[TW], i32x8 (&fx)[TX]) {
+            const unsigned char* st = smem + (slab & 1) * STAGE;
+            const int key = l32 >> 1 & 7;
+            auto frag = [&](const unsigned char* row) {
+                const u32x4 lo = *reinterpret_cast<const u32x4*>(row + (((ks * 4 + half) ^ key) << 4));
+                const u32x4 hi = *reinterpret_cast<const u32x4*>(row + (((ks * 4 + 2 + half) ^ key) << 4));
+                return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+            };
+#pragma unroll
+            for (int i = 0; i < TW; ++i) fw[i] = frag(st + (BX + (ww * TW + i) * 32 + l32) * 128);
+#pragma unroll
+            for (int j = 0; j < TX; ++j) fx[j] = frag(st + ((wx * TX + j) * 32 + l32) * 128);
+        };
+        auto read_scales = [&](int slab, int (&sw)[TW], int (&sx)[TX]) {     // this half's bytes 0 (first k-step) and 2 (second)
+            const int* st = reinterpret_cast<const int*>(smem + (slab & 1) * STAGE + ROWS * 128);
+#pragma unroll
+            for (int i = 0; i < TW; ++i) sw[i] = (int)((uint32_t)st[BX + (ww * TW + i) * 32 + l32] >> (8 * half));
+#pragma unroll
+            for (int j = 0; j < TX; ++j) sx[j] = (int)((uint32_t)st[(wx * TX + j) * 32 + l32] >> (8 * half));
+        };
+
+        f32x16 acc[TW][TX];
+#pragma unroll
+        for (int i = 0; i < TW; ++i)
+#pragma unroll
+            for (int j = 0; j < TX; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+        i32x8 w0[TW], x0[TX], w1[TW], x1[TX];
+        int sw[TW], sx[TX], sw2[TW], sx2[TX];
+        issue(0);
+        if (nslab > 1) { issue(1); wait_vmcnt<XLD + WLD + SLD>(); }
+        else wait_vmcnt<0>();
+        block_sync_lds();
+        read(0, 0, w0, x0);
+        read_scales(0, sw, sx);
+        for (int s = 0; s < nslab; ++s) {
+            read(s, 1, w1, x1);
+#pragma unroll
+            for (int j = 0; j < TX; ++j)
+#pragma unroll
+                for (int i = 0; i < TW; ++i) acc[i][j] = mfma32<0>(w0[i], x0[j], acc[i][j], sw[i], sx[j]);
+            if (s + 1 < nslab) {
+                wait_vmcnt<0>();
+                block_sync_lds();                             // slab s + 1 is there, and everybody has slab s in registers
+                if (s + 2 < nslab) issue(s + 2);
+                read(s + 1, 0, w0, x0);
+                read_scales(s + 1, sw2, sx2);
+            }
+#pragma unroll
+            for (int j = 0; j < TX; ++j)
+#pragma unroll
+                for (int i = 0; i < TW; ++i) acc[i][j] = mfma32<2>(w1[i], x1[j], acc[i][j], sw[i], sx[j]);
+#pragma unroll
+            for (int i = 0; i < TW; ++i) sw[i] = sw2[i];
+#pragma unroll
+            for (int j = 0; j < TX; ++j) sx[j] = sx2[j];
+        }
+
+        // ---- epilogue: lane = row, registers = columns; stores end where the tile's rows do ----
+#pragma unroll
+        for (int i = 0; i < TW; ++i) {
+            const int n = n0 + (ww * TW + i) * 32;            // N is a multiple of 32
+            if (n >= p.N) break;
+            float bias[16];
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                bias[r] = p.bias ? p.bias[(int64_t)g * p.N + n + 8 * (r >> 2) + 4 * half + (r & 3)] : 0.f;
+#pragma unroll
+            for (int j = 0; j < TX; ++j) {
+                const int r0 = (wx * TX + j) * 32, there = min(32, max(0, rows - r0));
+                const int64_t at = (int64_t)(row0 + r0);
+                float v[16];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) v[r] = acc[i][j][r] + bias[r];
+                if constexpr (FIRST) {
+                    float m = 0.f;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        v[r] = p.act == EVOMOE_RELU ? relu(v[r]) : gelu5(v[r]);
+                        m = fmaxf(m, mx_magnitude(v[r]));
+                    }
+                    uint32_t ma = __float_as_uint(m), mb = ma;
+                    swap_halves(ma, mb);
+                    const uint32_t b = mx_scale_byte(fmaxf(__uint_as_float(ma), __uint_as_float(mb)));
+                    const float inv = mx_inverse(b);
+                    uint32_t d[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) d[q] = mx_pack4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3], inv);
+                    swap_halves(d[0], d[2]);                  // the lower lanes get columns 0 .. 15, the upper ones 16 .. 31
+                    swap_halves(d[1], d[3]);
+                    __builtin_amdgcn_raw_buffer_store_b128(u32x4{d[0], d[2], d[1], d[3]}, rows_of(p.Aq + at * p.N, there * p.N),
+                                                           l32 * p.N + n + 16 * half, 0, 0);
+                    const int ng = p.N / kMxGroup;
+                    __builtin_amdgcn_raw_buffer_store_b8((uint8_t)b, rows_of(p.As + at * ng, there * ng),
+                                                         half ? 0x40000000 : l32 * ng + n / kMxGroup, 0, 0);
+                } else {
+                    uint32_t d[8];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) d[q] = pack_bf16x2(v[2 * q], v[2 * q + 1]);
+                    swap_halves(d[0], d[4]); swap_halves(d[1], d[5]); swap_halves(d[2], d[6]); swap_halves(d[3], d[7]);
+                    const auto to = rows_of(p.O + at * p.N, there * p.N * 2);
+                    const uint32_t off = (l32 * p.N + n + 16 * half) * 2;
+                    __builtin_amdgcn_raw_buffer_store_b128(u32x4{d[0], d[1], d[4], d[5]}, to, off, 0, 0);
+                    __builtin_amdgcn_raw_buffer_store_b128(u32x4{d[2], d[3], d[6], d[7]}, to, off + 16, 0, 0);
+                }
+            }
+        }
+    }
+}
+
+template <bool FIRST> hipError_t launch_small(const Ctx& c, const evomoe_shape& s, const Mx8Args& a) {
     const dim3 grid((unsigned)((s.P_cap + 15) / 16 + s.E), (unsigned)(a.N / 32));
     hipLaunchKernelGGL(mx8_gemm_kernel<FIRST>, grid, dim3(64), 0, c.stream, a);
     return hipGetLastError();
+}
+
+struct Big { static constexpr int BX = 256, BW = 256, WX = 2, WW = 2, WPE = 1; };
+struct Mid { static constexpr int BX = 128, BW = 128, WX = 2, WW = 2, WPE = 2; };
+
+template <bool FIRST, class Cfg> hipError_t launch_tiles(const Ctx& c, const evomoe_shape& s, const Mx8Args& a) {
+    auto kern = mx8_tile_kernel<FIRST, Cfg::BX, Cfg::BW, Cfg::WX, Cfg::WW, Cfg::WPE>;
+    constexpr int smem = 2 * (Cfg::BX + Cfg::BW) * 132;
+    static bool configured[kMaxDevices];
+    if (c.device < 0 || c.device >= kMaxDevices) return hipErrorInvalidDevice;
+    if (!configured[c.device]) {
+        hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != hipSuccess) return e;
+        configured[c.device] = true;
+    }
+    const int nct = (a.N + Cfg::BW - 1) / Cfg::BW;
+    const int64_t worst = ((s.P_cap + Cfg::BX - 1) / Cfg::BX + s.E) * nct, cap = (int64_t)c.num_cu * Cfg::WPE;
+    const int64_t fit = (int64_t)(2.4 * 1024 * 1024) / ((int64_t)Cfg::BW * a.K);
+    const int col_group = (int64_t)Cfg::BX * a.K >= (1 << 20) ? nct : (int)(fit < 1 ? 1 : fit > nct ? nct : fit);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(worst < cap ? worst : cap)), dim3(Cfg::WX * Cfg::WW * 64), smem, c.stream, a, col_group);
+    return hipGetLastError();
+}
+
+template <bool FIRST> hipError_t launch(const Ctx& c, const evomoe_shape& s, const Mx8Args& a) {
+    const int64_t pairs = c.pair_hint > 0 && c.pair_hint < s.P_cap ? c.pair_hint : s.P_cap;
+    if (a.K % 128 || pairs < 32 * s.E) return launch_small<FIRST>(c, s, a);
+    const int64_t tiles = ((pairs + 255) / 256 + s.E / 2) * ((a.N + 255) / 256);
+    return tiles >= 2 * c.num_cu ? launch_tiles<FIRST, Big>(c, s, a) : launch_tiles<FIRST, Mid>(c, s, a);
 }
 
 size_t aq_bytes(const evomoe_shape& s) { return ((size_t)s.P_cap * s.F + 255) & ~(size_t)255; }
