@@ -83,17 +83,14 @@ __global__ __launch_bounds__(64) void mx8_gemm_kernel(Mx8Args p)
         if (FIRST) v[j] = act_fwd(v[j], p.act);
     }
     if constexpr (FIRST) {
-        float m = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) m = fmaxf(m, mx_magnitude(v[j]));
+        float m = mx_largest(v);
         m = fmaxf(m, __shfl_xor(m, 16, 64));
         m = fmaxf(m, __shfl_xor(m, 32, 64));
         const uint32_t b = mx_scale_byte(m);
-        const float inv = mx_inverse(b);
         if (i16 < rows) {
             uint8_t* out = p.Aq + (int64_t)(row0 + i16) * p.N + n0 + 4 * q;
-            *reinterpret_cast<uint32_t*>(out) = mx_pack4(v[0], v[1], v[2], v[3], inv);
-            *reinterpret_cast<uint32_t*>(out + 16) = mx_pack4(v[4], v[5], v[6], v[7], inv);
+            *reinterpret_cast<uint32_t*>(out) = mx_pack4(v[0], v[1], v[2], v[3], b);
+            *reinterpret_cast<uint32_t*>(out + 16) = mx_pack4(v[4], v[5], v[6], v[7], b);
             if (q == 0) p.As[(int64_t)(row0 + i16) * (p.N / kMxGroup) + n0 / kMxGroup] = (uint8_t)b;
         }
     } else if (i16 < rows) {
@@ -114,7 +111,7 @@ __device__ __forceinline__ float gelu5(float h) {
     p = fmaf(p, x, -0.459992439f);
     p = fmaf(p, x, -1.15078785f);
     p = fmaf(p, x, -1.00003762f);
-    return fmaf(-x, __builtin_amdgcn_exp2f(p), relu(h));
+    return fmaf(-x, __builtin_amdgcn_exp2f(p), fmaxf(h, 0.f));       // (of a NaN the exponential is one)
 }
 
 // v_mfma_scale_f32_32x32x64_f8f6f4: lane (h = lane / 32, i = lane % 32) brings the k's 16 h .. 16 h + 15 and 32 + 16 h .. of row i of
@@ -131,25 +128,29 @@ __device__ __forceinline__ void swap_halves(uint32_t& a, uint32_t& b) {
     b = v[1];
 }
 
-// The tile kernel, for contractions that are a multiple of 128.  A block of WX x WW waves computes BX rows of X by BW rows of W, a
+// The tile kernel, for d and F that are multiples of 128.  A block of WX x WW waves computes BX rows of X by BW rows of W, a
 // wave TX x TW matrix instructions of 32 x 32.  The contraction runs in slabs of 128 bytes (one line of every row), two LDS stages
 // deep; a stage holds both operands' slabs, rows of 128 bytes with the 16-byte chunk c of row r at chunk c ^ (r >> 1 & 7), so that
 // sixteen lanes' reads of one chunk column meet all banks, and the four scale bytes of every row.  Loads go straight to the LDS.
 // Slab s + 2 is fetched into slab s's stage as soon as its last fragments are in registers, and lands while one and a half
 // slabs multiply.  Blocks are persistent and walk the tiles as the bf16 kernels do: expert by expert, column group by column
 // group, row tile by row tile, every XCD on a run of its own.
-template <bool FIRST, int BX, int BW, int WX, int WW, int WPE>
+// EPI: what becomes of the sums.
+enum { TO_RELU = EVOMOE_RELU, TO_GELU = EVOMOE_GELU_ERF, TO_OUTPUT };
+template <int EPI, int BX, int BW, int WX, int WW, int WPE>
 __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, int col_group)
 {
+    constexpr bool FIRST = EPI != TO_OUTPUT;
     constexpr int NW = WX * WW, TX = BX / WX / 32, TW = BW / WW / 32;
     constexpr int XLD = BX / 8 / NW, WLD = BW / 8 / NW;         // 1 KB load instructions per wave and slab
     constexpr int ROWS = BX + BW, SLD = ROWS / 64 / NW;         // scale load instructions per wave and slab (64 rows each)
     constexpr int STAGE = ROWS * 132;
+    static_assert(TW == 2 || TW == 4, "a row's scale bytes of a wave leave together");
     static_assert(XLD * 8 * NW == BX && WLD * 8 * NW == BW && SLD * 64 * NW == ROWS && BX % 64 == 0, "whole instructions");
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ int offs[65], tstart[65];
 
-    const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wx = wave / WW, ww = wave % WW;
     if (wave == 0) {          // lane e: expert e's rows, and the row tiles before it
@@ -181,171 +182,272 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
         step = gridDim.x;
     }
 
-    for (; seq < seq_end; seq += step) {
-        // ---- where the tile lies ----
-        int g, row0, rows, n0;
-        {
-            const int first = tstart[lane], next = tstart[lane + 1], begin = offs[lane], end = offs[lane + 1];
-            g = __popcll(__ballot(seq >= next * nct));
-            const int t0 = __builtin_amdgcn_readlane(first, g), nrt = __builtin_amdgcn_readlane(next, g) - t0;
-            const int r = seq - t0 * nct, cg = r / (nrt * col_group), r2 = r - cg * nrt * col_group;
-            const int gc = min(col_group, nct - cg * col_group), rt = r2 / gc;
-            n0 = (cg * col_group + (r2 - rt * gc)) * BW;
-            row0 = __builtin_amdgcn_readlane(begin, g) + rt * BX;
-            rows = min(BX, __builtin_amdgcn_readlane(end, g) - row0);
-        }
-        g = __builtin_amdgcn_readfirstlane(g);
-        n0 = __builtin_amdgcn_readfirstlane(n0);
-        row0 = __builtin_amdgcn_readfirstlane(row0);
-        rows = __builtin_amdgcn_readfirstlane(rows);
-
-        // ---- addresses: rows beyond the tile repeat its last one, their products are not stored ----
-        const unsigned char* xb = p.X + (p.rows ? (int64_t)0 : (int64_t)row0 * p.K);
-        const unsigned char* xsb = p.Xs + (p.rows ? (int64_t)0 : (int64_t)row0 * kg);
-        const unsigned char* wb = p.W + ((int64_t)g * p.N + n0) * p.K;
-        const unsigned char* wsb = p.Ws + ((int64_t)g * p.N + n0) * kg;
-        uint32_t xo[XLD], wo[WLD], so[SLD];
-        const int lr = lane >> 3;                              // this lane's row of the eight that an instruction brings
-        auto x_row = [&](int r) { const int c = min(r, rows - 1); return p.rows ? (uint32_t)p.rows[row0 + c] : (uint32_t)c; };
+    // What depends on the lane is made again for every tile's parts from a copy of the lane number that the compiler cannot see through:
+    // the values then do not occupy registers through the parts that do not use them.
+    auto fresh_lane = [&] { int v = lane; asm volatile("" : "+v"(v)); return v; };
+    // ---- a tile: where it lies, and its operands' addresses.  Rows beyond it repeat its last one, their products are not stored ----
+    struct Tile { int g, row0, rows, n0; };
+    auto locate = [&](int at) {
+        const int e = fresh_lane(), first = tstart[e], next = tstart[e + 1], begin = offs[e], end = offs[e + 1];
+        Tile t;
+        t.g = __popcll(__ballot(at >= next * nct));
+        const int t0 = __builtin_amdgcn_readlane(first, t.g), nrt = __builtin_amdgcn_readlane(next, t.g) - t0;
+        const int r = at - t0 * nct, cg = r / (nrt * col_group), r2 = r - cg * nrt * col_group;
+        const int gc = min(col_group, nct - cg * col_group), rt = r2 / gc;
+        t.n0 = __builtin_amdgcn_readfirstlane((cg * col_group + (r2 - rt * gc)) * BW);
+        t.row0 = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_readlane(begin, t.g) + rt * BX);
+        t.rows = __builtin_amdgcn_readfirstlane(min(BX, __builtin_amdgcn_readlane(end, t.g) - t.row0));
+        t.g = __builtin_amdgcn_readfirstlane(t.g);
+        return t;
+    };
+    // the rows of X that this lane brings: XLD for the data (row lane / 8 of an instruction's eight), then SLD for the scales
+    auto x_rows = [&](const Tile& t, uint32_t (&xr)[XLD + SLD]) {
+        const int lane = fresh_lane();
 #pragma unroll
-        for (int i = 0; i < XLD; ++i) {
-            const int r = (wave + NW * i) * 8 + lr;
-            xo[i] = x_row(r) * (uint32_t)p.K + (((lane & 7) ^ (r >> 1 & 7)) << 4);
-        }
+        for (int i = 0; i < XLD + SLD; ++i)
+            xr[i] = (uint32_t)min(i < XLD ? (wave + NW * i) * 8 + (lane >> 3) : (wave + NW * (i - XLD)) * 64 + lane, t.rows - 1);
+        if (p.rows) {
+            const int32_t* from = p.rows + t.row0;
 #pragma unroll
-        for (int i = 0; i < WLD; ++i) {
-            const int r = (wave + NW * i) * 8 + lr;
-            wo[i] = (uint32_t)min(r, p.N - 1 - n0) * (uint32_t)p.K + (((lane & 7) ^ (r >> 1 & 7)) << 4);
+            for (int i = 0; i < XLD + SLD; ++i) xr[i] = (uint32_t)from[xr[i]];
         }
+    };
+    const unsigned char *xb = nullptr, *xsb = nullptr, *wb = nullptr, *wsb = nullptr;
+    uint32_t xo[XLD], wo[WLD], so[SLD];
+    static_assert(NW % 2 == 0, "chunk");
+    auto aim = [&](const Tile& t, const uint32_t (&xr)[XLD + SLD]) {
+        const int lane = fresh_lane();
+        // (an instruction's eight rows begin at a multiple of 8 and NW is even: the chunk that a lane brings is the same in all of them)
+        const uint32_t chunk = (uint32_t)(((lane & 7) ^ ((wave * 8 + (lane >> 3)) >> 1 & 7)) << 4);
+        xb = p.X + (p.rows ? (int64_t)0 : (int64_t)t.row0 * p.K);
+        xsb = p.Xs + (p.rows ? (int64_t)0 : (int64_t)t.row0 * kg);
+        wb = p.W + ((int64_t)t.g * p.N + t.n0) * p.K;
+        wsb = p.Ws + ((int64_t)t.g * p.N + t.n0) * kg;
+        const int last = p.N - 1 - t.n0;
+#pragma unroll
+        for (int i = 0; i < XLD; ++i) xo[i] = xr[i] * (uint32_t)p.K + chunk;
+#pragma unroll
+        for (int i = 0; i < WLD; ++i) wo[i] = (uint32_t)min((wave + NW * i) * 8 + (lane >> 3), last) * (uint32_t)p.K + chunk;
 #pragma unroll
         for (int i = 0; i < SLD; ++i) {
-            const int r = (wave + NW * i) * 64 + lane;        // X's rows, then W's
-            so[i] = (r < BX ? x_row(r) : (uint32_t)min(r - BX, p.N - 1 - n0)) * (uint32_t)kg;
+            const int r = (wave + NW * i) * 64;               // X's rows, then W's; 64 of one operand, as BX is a multiple of 64
+            so[i] = (r < BX ? xr[XLD + i] : (uint32_t)min(r + lane - BX, last)) * (uint32_t)kg;
         }
-        // (what the compiler itself has loaded so far is complete, and known to be, before the loads that it does not count begin)
-        __builtin_amdgcn_s_waitcnt(0x0f70);                   // vmcnt(0)
-        block_sync_lds();                                     // the previous tile's readers are done with both stages
-        auto issue = [&](int slab) {
-            unsigned char* st = smem + (slab & 1) * STAGE;
+    };
+    // load instruction number x of a slab: X's rows, W's rows, scales
+    constexpr int NLD = XLD + WLD + SLD;
+    auto issue_one = [&](int x, int slab) {
+        unsigned char* st = smem + (slab & 1) * STAGE;
+        if (x < XLD) {
+            load_to_lds(xb + slab * 128, xo[x], st + (wave + NW * x) * 1024);
+        } else if (x < XLD + WLD) {
+            const int i = x - XLD;
+            load_to_lds(wb + slab * 128, wo[i], st + BX * 128 + (wave + NW * i) * 1024);
+        } else {
+            const int i = x - XLD - WLD, r = (wave + NW * i) * 64;
+            load_dword_to_lds(reinterpret_cast<const int32_t*>((r < BX ? xsb : wsb) + slab * 4), so[i],
+                              reinterpret_cast<const int*>(st + ROWS * 128 + r * 4));
+        }
+    };
+    auto issue = [&](int slab) {
 #pragma unroll
-            for (int i = 0; i < XLD; ++i) load_to_lds(xb, xo[i] + slab * 128, st + (wave + NW * i) * 1024);
-#pragma unroll
-            for (int i = 0; i < WLD; ++i) load_to_lds(wb, wo[i] + slab * 128, st + BX * 128 + (wave + NW * i) * 1024);
-#pragma unroll
-            for (int i = 0; i < SLD; ++i) {
-                const int r = (wave + NW * i) * 64;           // (64 rows of one operand: BX is a multiple of 64)
-                load_dword_to_lds(reinterpret_cast<const int32_t*>(r < BX ? xsb : wsb), so[i] + slab * 4,
-                                  reinterpret_cast<const int*>(st + ROWS * 128 + r * 4));
-            }
-        };
-        auto read = [&](int slab, int ks, i32x8 (&fw)[TW], i32x8 (&fx)[TX]) {
+        for (int x = 0; x < NLD; ++x) issue_one(x, slab);
+    };
+    // a tile's bias (zeros, where there is none) and its first two slabs
+    float* const bias_lds = reinterpret_cast<float*>(smem + 2 * STAGE);       // [2][BW], by the tile's parity
+    auto begin = [&](const Tile& t, int parity) {
+        if (p.bias) {
+            const int i = wave % (BW / 64) * 64;
+            load_dword_to_lds(reinterpret_cast<const int32_t*>(p.bias + (int64_t)t.g * p.N), (uint32_t)min(t.n0 + i + lane, p.N - 1) * 4,
+                              reinterpret_cast<const int*>(bias_lds + parity * BW + i));
+        }
+        issue(0);
+        if (nslab > 1) issue(1);
+    };
+
+    if (!p.bias)
+        for (int i = threadIdx.x; i < 2 * BW; i += NW * 64) bias_lds[i] = 0.f;
+    if (seq >= seq_end) return;
+    Tile t = locate(seq);
+    {
+        uint32_t xr[XLD + SLD];
+        x_rows(t, xr);
+        aim(t, xr);
+        __builtin_amdgcn_s_waitcnt(0x0f70);       // vmcnt(0): what the compiler itself has loaded is complete before the loads it does not count
+        begin(t, 0);
+    }
+    // a wave's stores in an epilogue, at least: they follow the next tile's first loads, and are not waited for with them
+    constexpr int STORES = TX * (FIRST ? TW + 1 : 2 * TW);
+    static_assert(NLD + STORES <= 63, "vmcnt");
+    bool first = true;
+    for (int parity = 0;; parity ^= 1) {
+        const int lane_t = fresh_lane(), l32 = lane_t & 31, half = lane_t >> 5, key = l32 >> 1 & 7;
+        // fragment number f (W's, then X's) of k-step ks
+        auto read_one = [&](int f, int slab, int ks, i32x8 (&fw)[TW], i32x8 (&fx)[TX]) {
             const unsigned char* st = smem + (slab & 1) * STAGE;
-            const int key = l32 >> 1 & 7;
-            auto frag = [&](const unsigned char* row) {
-                const u32x4 lo = *reinterpret_cast<const u32x4*>(row + (((ks * 4 + half) ^ key) << 4));
-                const u32x4 hi = *reinterpret_cast<const u32x4*>(row + (((ks * 4 + 2 + half) ^ key) << 4));
-                return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
-            };
-#pragma unroll
-            for (int i = 0; i < TW; ++i) fw[i] = frag(st + (BX + (ww * TW + i) * 32 + l32) * 128);
-#pragma unroll
-            for (int j = 0; j < TX; ++j) fx[j] = frag(st + ((wx * TX + j) * 32 + l32) * 128);
+            const unsigned char* row = st + (f < TW ? BX + (ww * TW + f) * 32 + l32 : (wx * TX + f - TW) * 32 + l32) * 128;
+            const u32x4 lo = *reinterpret_cast<const u32x4*>(row + (((ks * 4 + half) ^ key) << 4));
+            const u32x4 hi = *reinterpret_cast<const u32x4*>(row + (((ks * 4 + 2 + half) ^ key) << 4));
+            (f < TW ? fw[f < TW ? f : 0] : fx[f < TW ? 0 : f - TW]) =
+                i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
         };
-        auto read_scales = [&](int slab, int (&sw)[TW], int (&sx)[TX]) {     // this half's bytes 0 (first k-step) and 2 (second)
+        auto read_scales = [&](int slab, int (&sw)[TW], int (&sx)[TX]) {
             const int* st = reinterpret_cast<const int*>(smem + (slab & 1) * STAGE + ROWS * 128);
 #pragma unroll
-            for (int i = 0; i < TW; ++i) sw[i] = (int)((uint32_t)st[BX + (ww * TW + i) * 32 + l32] >> (8 * half));
+            for (int i = 0; i < TW; ++i) sw[i] = st[BX + (ww * TW + i) * 32 + l32];
 #pragma unroll
-            for (int j = 0; j < TX; ++j) sx[j] = (int)((uint32_t)st[(wx * TX + j) * 32 + l32] >> (8 * half));
+            for (int j = 0; j < TX; ++j) sx[j] = st[(wx * TX + j) * 32 + l32];
         };
-
         f32x16 acc[TW][TX];
+        i32x8 w0[TW], x0[TX], w1[TW], x1[TX];
+        int sw[TW], sx[TX], sw_next[TW], sx_next[TX];
+        // One k-step (64 k's): its matrix instructions, and between them, pinned there, the reads of the next k-step's fragments (the
+        // first half of the instructions take them) and a later slab's loads.
+        auto kstep = [&](auto op, auto begins, const i32x8 (&fw)[TW], const i32x8 (&fx)[TX], auto&& between) {
+            constexpr int NMF = TW * TX;
+#pragma unroll
+            for (int m = 0; m < NMF; ++m) {
+                const int j = m / TW, i = m % TW;
+                acc[i][j] = mfma32<decltype(op)::value>(fw[i], fx[j], decltype(begins)::value ? f32x16{} : acc[i][j], sw[i], sx[j]);
+                between(m, NMF);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        constexpr int NFR = TW + TX;
+        auto read_share = [&](int m, int n, int slab, int ks, i32x8 (&fw)[TW], i32x8 (&fx)[TX]) {
+            const int h = n / 2;
+            if (m >= h) return;
+#pragma unroll
+            for (int f = NFR * m / h; f < NFR * (m + 1) / h; ++f) read_one(f, slab, ks, fw, fx);
+        };
+        auto use_scales = [&](const int (&w)[TW], const int (&x)[TX]) {       // this half's bytes: 0 (first k-step) and 2 (second)
+#pragma unroll
+            for (int i = 0; i < TW; ++i) sw[i] = (int)((uint32_t)w[i] >> (8 * half));
+#pragma unroll
+            for (int j = 0; j < TX; ++j) sx[j] = (int)((uint32_t)x[j] >> (8 * half));
+        };
+        if (nslab == 1) wait_vmcnt<0>();
+        else if (first) wait_vmcnt<NLD>();
+        else wait_vmcnt<NLD + STORES>();
+        first = false;
+        block_sync_lds();
+#pragma unroll
+        for (int f = 0; f < NFR; ++f) read_one(f, 0, 0, w0, x0);
+        read_scales(0, sw_next, sx_next);
+        use_scales(sw_next, sx_next);
+        constexpr auto OP0 = std::integral_constant<int, 0>{};
+        constexpr auto OP2 = std::integral_constant<int, 2>{};
+        auto first_half = [&](int s, auto begins) {
+            kstep(OP0, begins, w0, x0, [&](int m, int n) { read_share(m, n, s, 1, w1, x1); });
+        };
+        auto second_half = [&](int s, auto more) {            // of a slab that has a next; more: which has a next as well
+            wait_vmcnt<0>();
+            block_sync_lds();                                 // slab s + 1 is there, and everybody has slab s in registers
+            kstep(OP2, std::false_type{}, w1, x1, [&](int m, int n) {
+                if (m == 0) read_scales(s + 1, sw_next, sx_next);
+                read_share(m, n, s + 1, 0, w0, x0);
+                if (decltype(more)::value) {
+#pragma unroll
+                    for (int x = NLD * m / n; x < NLD * (m + 1) / n; ++x) issue_one(x, s + 2);
+                }
+            });
+            use_scales(sw_next, sx_next);
+        };
+        first_half(0, std::true_type{});
+        int s = 0;
+        for (; s + 2 < nslab; ++s) {
+            second_half(s, std::true_type{});
+            first_half(s + 1, std::false_type{});
+        }
+        // the next tile's row numbers arrive under the last slabs
+        const bool more_tiles = seq + step < seq_end;
+        Tile next = t;
+        if (more_tiles) next = locate(seq + step);
+        if (s + 1 < nslab) {
+            second_half(s, std::false_type{});
+            first_half(s + 1, std::false_type{});
+        }
+        uint32_t xr[XLD + SLD];
+        x_rows(next, xr);
+        kstep(OP2, std::false_type{}, w1, x1, [&](int, int) {});
+        // (the compiler would move these matrix instructions down to where their sums are read, and keep their operands until there)
+        auto pin = [](f32x16& sums) {
+            if constexpr (TW * TX * 16 > 128) asm volatile("" : "+a"(sums));
+            else asm volatile("" : "+v"(sums));
+        };
 #pragma unroll
         for (int i = 0; i < TW; ++i)
 #pragma unroll
-            for (int j = 0; j < TX; ++j)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-        i32x8 w0[TW], x0[TX], w1[TW], x1[TX];
-        int sw[TW], sx[TX], sw2[TW], sx2[TX];
-        issue(0);
-        if (nslab > 1) { issue(1); wait_vmcnt<XLD + WLD + SLD>(); }
-        else wait_vmcnt<0>();
-        block_sync_lds();
-        read(0, 0, w0, x0);
-        read_scales(0, sw, sx);
-        for (int s = 0; s < nslab; ++s) {
-            read(s, 1, w1, x1);
-#pragma unroll
-            for (int j = 0; j < TX; ++j)
-#pragma unroll
-                for (int i = 0; i < TW; ++i) acc[i][j] = mfma32<0>(w0[i], x0[j], acc[i][j], sw[i], sx[j]);
-            if (s + 1 < nslab) {
-                wait_vmcnt<0>();
-                block_sync_lds();                             // slab s + 1 is there, and everybody has slab s in registers
-                if (s + 2 < nslab) issue(s + 2);
-                read(s + 1, 0, w0, x0);
-                read_scales(s + 1, sw2, sx2);
-            }
-#pragma unroll
-            for (int j = 0; j < TX; ++j)
-#pragma unroll
-                for (int i = 0; i < TW; ++i) acc[i][j] = mfma32<2>(w1[i], x1[j], acc[i][j], sw[i], sx[j]);
-#pragma unroll
-            for (int i = 0; i < TW; ++i) sw[i] = sw2[i];
-#pragma unroll
-            for (int j = 0; j < TX; ++j) sx[j] = sx2[j];
+            for (int j = 0; j < TX; ++j) pin(acc[i][j]);
+        block_sync_lds();                                     // everybody is done with both stages
+        if (more_tiles) {
+            aim(next, xr);
+            __builtin_amdgcn_s_waitcnt(0x0f70);               // vmcnt(0), as above
+            begin(next, parity ^ 1);
         }
 
-        // ---- epilogue: lane = row, registers = columns; stores end where the tile's rows do ----
-#pragma unroll
-        for (int i = 0; i < TW; ++i) {
-            const int n = n0 + (ww * TW + i) * 32;            // N is a multiple of 32
-            if (n >= p.N) break;
-            float bias[16];
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                bias[r] = p.bias ? p.bias[(int64_t)g * p.N + n + 8 * (r >> 2) + 4 * half + (r & 3)] : 0.f;
+        // ---- epilogue: lane = row, registers = columns; stores end where the tile's rows do, and are made without a branch (a matrix
+        // instruction whose result only some lanes use may be moved under their branch, where the others bring no operands) ----
+        {
+            const int lane_e = fresh_lane(), l32 = lane_e & 31, half = lane_e >> 5;
 #pragma unroll
             for (int j = 0; j < TX; ++j) {
-                const int r0 = (wx * TX + j) * 32, there = min(32, max(0, rows - r0));
-                const int64_t at = (int64_t)(row0 + r0);
-                float v[16];
+                const int r0 = (wx * TX + j) * 32, there = min(32, max(0, t.rows - r0));
+                const int64_t at = (int64_t)(t.row0 + r0);
+                uint32_t bytes[TW];
 #pragma unroll
-                for (int r = 0; r < 16; ++r) v[r] = acc[i][j][r] + bias[r];
-                if constexpr (FIRST) {
-                    float m = 0.f;
+                for (int i = 0; i < TW; ++i) {
+                    const int n = t.n0 + (ww * TW + i) * 32;  // N is a multiple of 32
+                    const uint32_t beyond = n < p.N ? 0u : 0x40000000u;
+                    pin(acc[i][j]);                           // (one unit's sums in vector registers at a time)
+                    float v[16];
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        v[r] = p.act == EVOMOE_RELU ? relu(v[r]) : gelu5(v[r]);
-                        m = fmaxf(m, mx_magnitude(v[r]));
+                    for (int r = 0; r < 16; ++r) v[r] = acc[i][j][r];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x4 b = *reinterpret_cast<const f32x4*>(bias_lds + parity * BW + (ww * TW + i) * 32 + 8 * q + 4 * half);
+                        v[4 * q] += b.x; v[4 * q + 1] += b.y; v[4 * q + 2] += b.z; v[4 * q + 3] += b.w;
                     }
-                    uint32_t ma = __float_as_uint(m), mb = ma;
-                    swap_halves(ma, mb);
-                    const uint32_t b = mx_scale_byte(fmaxf(__uint_as_float(ma), __uint_as_float(mb)));
-                    const float inv = mx_inverse(b);
-                    uint32_t d[4];
+                    if constexpr (FIRST) {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) d[q] = mx_pack4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3], inv);
-                    swap_halves(d[0], d[2]);                  // the lower lanes get columns 0 .. 15, the upper ones 16 .. 31
-                    swap_halves(d[1], d[3]);
-                    __builtin_amdgcn_raw_buffer_store_b128(u32x4{d[0], d[2], d[1], d[3]}, rows_of(p.Aq + at * p.N, there * p.N),
-                                                           l32 * p.N + n + 16 * half, 0, 0);
-                    const int ng = p.N / kMxGroup;
-                    __builtin_amdgcn_raw_buffer_store_b8((uint8_t)b, rows_of(p.As + at * ng, there * ng),
-                                                         half ? 0x40000000 : l32 * ng + n / kMxGroup, 0, 0);
-                } else {
-                    uint32_t d[8];
+                        for (int r = 0; r < 16; ++r) v[r] = EPI == TO_RELU ? relu(v[r]) : gelu5(v[r]);
+                        uint32_t ma = __float_as_uint(mx_max(v)), mb = ma;      // (of a group with an infinity any scale will do: O is NaN)
+                        swap_halves(ma, mb);
+                        const uint32_t b = mx_scale_byte(fmaxf(__uint_as_float(ma), __uint_as_float(mb)));
+                        bytes[i] = b;
+                        uint32_t d[4];
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) d[q] = pack_bf16x2(v[2 * q], v[2 * q + 1]);
-                    swap_halves(d[0], d[4]); swap_halves(d[1], d[5]); swap_halves(d[2], d[6]); swap_halves(d[3], d[7]);
-                    const auto to = rows_of(p.O + at * p.N, there * p.N * 2);
-                    const uint32_t off = (l32 * p.N + n + 16 * half) * 2;
-                    __builtin_amdgcn_raw_buffer_store_b128(u32x4{d[0], d[1], d[4], d[5]}, to, off, 0, 0);
-                    __builtin_amdgcn_raw_buffer_store_b128(u32x4{d[2], d[3], d[6], d[7]}, to, off + 16, 0, 0);
+                        for (int q = 0; q < 4; ++q) d[q] = mx_pack4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3], b);
+                        swap_halves(d[0], d[2]);              // the lower lanes get columns 0 .. 15, the upper ones 16 .. 31
+                        swap_halves(d[1], d[3]);
+                        __builtin_amdgcn_raw_buffer_store_b128(u32x4{d[0], d[2], d[1], d[3]}, rows_of(p.Aq + at * p.N, there * p.N),
+                                                               (l32 * p.N + n + 16 * half) | beyond, 0, 0);
+                    } else {
+                        uint32_t d[8];
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) d[q] = pack_bf16x2(v[2 * q], v[2 * q + 1]);
+                        swap_halves(d[0], d[4]); swap_halves(d[1], d[5]); swap_halves(d[2], d[6]); swap_halves(d[3], d[7]);
+                        const auto to = rows_of(p.O + at * p.N, there * p.N * 2);
+                        const uint32_t off = ((l32 * p.N + n + 16 * half) * 2) | beyond;
+                        __builtin_amdgcn_raw_buffer_store_b128(u32x4{d[0], d[1], d[4], d[5]}, to, off, 0, 0);
+                        __builtin_amdgcn_raw_buffer_store_b128(u32x4{d[2], d[3], d[6], d[7]}, to, off + 16, 0, 0);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if constexpr (FIRST) {
+                    const int ng = p.N / kMxGroup, n = (t.n0 + ww * TW * 32) / kMxGroup;
+                    const auto to = rows_of(p.As + at * ng, there * ng);
+                    const int off = half || n >= ng ? 0x40000000 : l32 * ng + n;       // (N is a multiple of a wave's columns)
+                    if constexpr (TW == 4)
+                        __builtin_amdgcn_raw_buffer_store_b32(bytes[0] | bytes[1] << 8 | bytes[2 % TW] << 16 | bytes[3 % TW] << 24, to, off, 0, 0);
+                    else
+                        __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(bytes[0] | bytes[1] << 8), to, off, 0, 0);
                 }
             }
         }
+        if (!more_tiles) break;
+        t = next;
+        seq += step;
     }
 }
 
@@ -358,9 +460,9 @@ template <bool FIRST> hipError_t launch_small(const Ctx& c, const evomoe_shape& 
 struct Big { static constexpr int BX = 256, BW = 256, WX = 2, WW = 2, WPE = 1; };
 struct Mid { static constexpr int BX = 128, BW = 128, WX = 2, WW = 2, WPE = 2; };
 
-template <bool FIRST, class Cfg> hipError_t launch_tiles(const Ctx& c, const evomoe_shape& s, const Mx8Args& a) {
-    auto kern = mx8_tile_kernel<FIRST, Cfg::BX, Cfg::BW, Cfg::WX, Cfg::WW, Cfg::WPE>;
-    constexpr int smem = 2 * (Cfg::BX + Cfg::BW) * 132;
+template <int EPI, class Cfg> hipError_t launch_tiles(const Ctx& c, const evomoe_shape& s, const Mx8Args& a) {
+    auto kern = mx8_tile_kernel<EPI, Cfg::BX, Cfg::BW, Cfg::WX, Cfg::WW, Cfg::WPE>;
+    constexpr int smem = 2 * (Cfg::BX + Cfg::BW) * 132 + 2 * Cfg::BW * 4;
     static bool configured[kMaxDevices];
     if (c.device < 0 || c.device >= kMaxDevices) return hipErrorInvalidDevice;
     if (!configured[c.device]) {
@@ -378,9 +480,14 @@ template <bool FIRST, class Cfg> hipError_t launch_tiles(const Ctx& c, const evo
 
 template <bool FIRST> hipError_t launch(const Ctx& c, const evomoe_shape& s, const Mx8Args& a) {
     const int64_t pairs = c.pair_hint > 0 && c.pair_hint < s.P_cap ? c.pair_hint : s.P_cap;
-    if (a.K % 128 || pairs < 32 * s.E) return launch_small<FIRST>(c, s, a);
+    if (s.d % 128 || s.F % 128 || pairs < 32 * s.E) return launch_small<FIRST>(c, s, a);
     const int64_t tiles = ((pairs + 255) / 256 + s.E / 2) * ((a.N + 255) / 256);
-    return tiles >= 2 * c.num_cu ? launch_tiles<FIRST, Big>(c, s, a) : launch_tiles<FIRST, Mid>(c, s, a);
+    auto run = [&](auto epi) {
+        constexpr int EPI = decltype(epi)::value;
+        return tiles >= 2 * c.num_cu ? launch_tiles<EPI, Big>(c, s, a) : launch_tiles<EPI, Mid>(c, s, a);
+    };
+    if (!FIRST) return run(std::integral_constant<int, TO_OUTPUT>{});
+    return a.act == EVOMOE_RELU ? run(std::integral_constant<int, TO_RELU>{}) : run(std::integral_constant<int, TO_GELU>{});
 }
 
 size_t aq_bytes(const evomoe_shape& s) { return ((size_t)s.P_cap * s.F + 255) & ~(size_t)255; }

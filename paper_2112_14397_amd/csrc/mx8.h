@@ -15,20 +15,33 @@ __device__ __forceinline__ uint32_t mx_scale_byte(float amax) {
     const int b = (int)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u);
     return (uint32_t)max(b, 0);
 }
-// 2^(127 - b), what values are multiplied by (exactly) before they are rounded; b <= 247 as amax is finite, so that the factor
-// is 2^-120 at least; 2^127 at most
-__device__ __forceinline__ float mx_inverse(uint32_t b) { return __uint_as_float((254u - b) << 23); }
-
-// magnitude for the group's maximum: infinities and NaNs count as 0
-__device__ __forceinline__ float mx_magnitude(float v) {
-    const float m = fabsf(v);
-    return m < INFINITY ? m : 0.f;
+// The largest magnitude of N values (the instruction passes a NaN over), and the largest finite one (an infinity, which is rare,
+// takes a second look).
+template <int N> __device__ __forceinline__ float mx_max(const float (&v)[N]) {
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; i += 2) m = fmaxf(fmaxf(fabsf(v[i]), fabsf(v[i + 1])), m);
+    return m;
 }
-// Four values -> four e4m3 bytes, round to nearest even (an infinity times the factor stays one, and the conversion makes it
-// and a NaN the NaN of e4m3, as nothing that is finite exceeds 448 here).
-__device__ __forceinline__ uint32_t mx_pack4(float a, float b, float c, float d, float inv) {
-    int v = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, v, true);
+template <int N> __device__ __forceinline__ float mx_largest(const float (&v)[N]) {
+    float m = mx_max(v);
+    if (m == INFINITY) {
+        m = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) m = fmaxf(m, fabsf(v[i]) < INFINITY ? fabsf(v[i]) : 0.f);
+    }
+    return m;
+}
+// Four values -> four e4m3 bytes, round to nearest even.  The instruction divides by the power of two in its scale operand's exponent
+// field, whose mantissa it does not look at; with the mantissa's first bit set a field of 0 is 2^-127 too.  What is finite stays
+// within 448; infinities and NaNs become the NaN of e4m3.
+__device__ __forceinline__ uint32_t mx_pack4(float a, float b, float c, float d, uint32_t scale_byte) {
+    typedef short s16x2 __attribute__((ext_vector_type(2)));
+    const float scale = __uint_as_float(scale_byte << 23 | 0x400000u);
+    s16x2 v = {0, 0};
+    v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, a, b, scale, false);
+    v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, c, d, scale, true);
+    return __builtin_bit_cast(uint32_t, v);
 }
 
 }  // namespace evomoe

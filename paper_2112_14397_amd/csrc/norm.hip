@@ -32,16 +32,13 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
 // One vector of a row, in 8 bits: the 32 / KV lanes of a group lie next to each other, and all of them or none are here.
 template <int KV>
 __device__ __forceinline__ void store_mx8(const float (&v)[KV], uint8_t* q, uint8_t* scale, int64_t at) {
-    float m = 0.f;
-#pragma unroll
-    for (int j = 0; j < KV; ++j) m = fmaxf(m, mx_magnitude(v[j]));
+    float m = mx_largest(v);
 #pragma unroll
     for (int o = 1; o < kMxGroup / KV; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
     const uint32_t b = mx_scale_byte(m);
-    const float inv = mx_inverse(b);
 #pragma unroll
     for (int j = 0; j < KV; j += 4)
-        *reinterpret_cast<uint32_t*>(q + at + j) = mx_pack4(v[j], v[j + 1], v[j + 2], v[j + 3], inv);
+        *reinterpret_cast<uint32_t*>(q + at + j) = mx_pack4(v[j], v[j + 1], v[j + 2], v[j + 3], b);
     if (at % kMxGroup == 0) scale[at / kMxGroup] = (uint8_t)b;
 }
 
