@@ -131,7 +131,9 @@ __device__ __forceinline__ void swap_halves(uint32_t& a, uint32_t& b) {
 // The tile kernel, for d and F that are multiples of 128.  A block of WX x WW waves computes BX rows of X by BW rows of W, a
 // wave TX x TW matrix instructions of 32 x 32.  The contraction runs in slabs of 128 bytes (one line of every row), two LDS stages
 // deep; a stage holds both operands' slabs, rows of 128 bytes with the 16-byte chunk c of row r at chunk c ^ (r >> 1 & 7), so that
-// sixteen lanes' reads of one chunk column meet all banks, and the four scale bytes of every row.  Loads go straight to the LDS.
+// sixteen lanes' reads of one chunk column meet all banks.  Scales come for four slabs at a time, 16 bytes of a row (with the loads of
+// the first of them), as every row lies in another line: slab by slab, 4 bytes of a row, they took as long as half of the data (65536 pairs, one
+// expert, d = 1024, F = 4096: second product 290 us, without loading scales 253).  Loads go straight to the LDS.
 // Slab s + 2 is fetched into slab s's stage as soon as its last fragments are in registers, and lands while one and a half
 // slabs multiply.  Blocks are persistent and walk the tiles as the bf16 kernels do: expert by expert, column group by column
 // group, row tile by row tile, every XCD on a run of its own.
@@ -143,8 +145,8 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
     constexpr bool FIRST = EPI != TO_OUTPUT;
     constexpr int NW = WX * WW, TX = BX / WX / 32, TW = BW / WW / 32;
     constexpr int XLD = BX / 8 / NW, WLD = BW / 8 / NW;         // 1 KB load instructions per wave and slab
-    constexpr int ROWS = BX + BW, SLD = ROWS / 64 / NW;         // scale load instructions per wave and slab (64 rows each)
-    constexpr int STAGE = ROWS * 132;
+    constexpr int ROWS = BX + BW, SLD = ROWS / 64 / NW;         // scale load instructions per wave (64 rows each)
+    constexpr int STAGE = ROWS * 128, SCALES = ROWS * 16;
     static_assert(TW == 2 || TW == 4, "a row's scale bytes of a wave leave together");
     static_assert(XLD * 8 * NW == BX && WLD * 8 * NW == BW && SLD * 64 * NW == ROWS && BX % 64 == 0, "whole instructions");
     extern __shared__ __align__(16) unsigned char smem[];
@@ -234,33 +236,46 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
             so[i] = (r < BX ? xr[XLD + i] : (uint32_t)min(r + lane - BX, last)) * (uint32_t)kg;
         }
     };
-    // load instruction number x of a slab: X's rows, W's rows, scales
-    constexpr int NLD = XLD + WLD + SLD;
+    // load instruction number x of a slab: X's rows, then W's
+    constexpr int NLD = XLD + WLD;
     auto issue_one = [&](int x, int slab) {
         unsigned char* st = smem + (slab & 1) * STAGE;
         if (x < XLD) {
             load_to_lds(xb + slab * 128, xo[x], st + (wave + NW * x) * 1024);
-        } else if (x < XLD + WLD) {
+        } else {
             const int i = x - XLD;
             load_to_lds(wb + slab * 128, wo[i], st + BX * 128 + (wave + NW * i) * 1024);
-        } else {
-            const int i = x - XLD - WLD, r = (wave + NW * i) * 64;
-            load_dword_to_lds(reinterpret_cast<const int32_t*>((r < BX ? xsb : wsb) + slab * 4), so[i],
-                              reinterpret_cast<const int*>(st + ROWS * 128 + r * 4));
+        }
+    };
+    // Scales, [2][ROWS][4 slabs' 4 bytes] by the parity of the four; the last four begin where they end with the row.  A contraction of
+    // fewer than four slabs has them slab by slab, [slab][ROWS].
+    unsigned char* const scales = smem + 2 * STAGE;
+    const bool by_four = nslab >= 4;
+    auto first_of = [&](int slab) { return min(slab & ~3, nslab - 4); };
+    auto issue_scales = [&](int slab) {
+#pragma unroll
+        for (int i = 0; i < SLD; ++i) {
+            const int r = (wave + NW * i) * 64;
+            const unsigned char* from = r < BX ? xsb : wsb;
+            if (by_four) load_to_lds(from + first_of(slab) * 4, so[i], scales + (slab >> 2 & 1) * SCALES + r * 16);
+            else
+                for (int u = 0; u < nslab; ++u)
+                    load_dword_to_lds(reinterpret_cast<const int32_t*>(from + u * 4), so[i], reinterpret_cast<const int*>(scales + (u * ROWS + r) * 4));
         }
     };
     auto issue = [&](int slab) {
 #pragma unroll
         for (int x = 0; x < NLD; ++x) issue_one(x, slab);
     };
-    // a tile's bias (zeros, where there is none) and its first two slabs
-    float* const bias_lds = reinterpret_cast<float*>(smem + 2 * STAGE);       // [2][BW], by the tile's parity
+    // a tile's bias (zeros, where there is none), its first scales and its first two slabs
+    float* const bias_lds = reinterpret_cast<float*>(scales + 2 * SCALES);    // [2][BW], by the tile's parity
     auto begin = [&](const Tile& t, int parity) {
         if (p.bias) {
             const int i = wave % (BW / 64) * 64;
             load_dword_to_lds(reinterpret_cast<const int32_t*>(p.bias + (int64_t)t.g * p.N), (uint32_t)min(t.n0 + i + lane, p.N - 1) * 4,
                               reinterpret_cast<const int*>(bias_lds + parity * BW + i));
         }
+        issue_scales(0);
         issue(0);
         if (nslab > 1) issue(1);
     };
@@ -292,11 +307,12 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
                 i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
         };
         auto read_scales = [&](int slab, int (&sw)[TW], int (&sx)[TX]) {
-            const int* st = reinterpret_cast<const int*>(smem + (slab & 1) * STAGE + ROWS * 128);
+            const int per_row = by_four ? 16 : 4;
+            const unsigned char* st = scales + (by_four ? (slab >> 2 & 1) * SCALES + (slab - first_of(slab)) * 4 : slab * ROWS * 4) + l32 * per_row;
 #pragma unroll
-            for (int i = 0; i < TW; ++i) sw[i] = st[BX + (ww * TW + i) * 32 + l32];
+            for (int i = 0; i < TW; ++i) sw[i] = *reinterpret_cast<const int*>(st + (BX + (ww * TW + i) * 32) * per_row);
 #pragma unroll
-            for (int j = 0; j < TX; ++j) sx[j] = st[(wx * TX + j) * 32 + l32];
+            for (int j = 0; j < TX; ++j) sx[j] = *reinterpret_cast<const int*>(st + (wx * TX + j) * 32 * per_row);
         };
         f32x16 acc[TW][TX];
         i32x8 w0[TW], x0[TX], w1[TW], x1[TX];
@@ -347,6 +363,7 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
                 if (m == 0) read_scales(s + 1, sw_next, sx_next);
                 read_share(m, n, s + 1, 0, w0, x0);
                 if (decltype(more)::value) {
+                    if (m == 0 && (s + 2) % 4 == 0) issue_scales(s + 2);
 #pragma unroll
                     for (int x = NLD * m / n; x < NLD * (m + 1) / n; ++x) issue_one(x, s + 2);
                 }
@@ -462,7 +479,7 @@ struct Mid { static constexpr int BX = 128, BW = 128, WX = 2, WW = 2, WPE = 2; }
 
 template <int EPI, class Cfg> hipError_t launch_tiles(const Ctx& c, const evomoe_shape& s, const Mx8Args& a) {
     auto kern = mx8_tile_kernel<EPI, Cfg::BX, Cfg::BW, Cfg::WX, Cfg::WW, Cfg::WPE>;
-    constexpr int smem = 2 * (Cfg::BX + Cfg::BW) * 132 + 2 * Cfg::BW * 4;
+    constexpr int smem = 2 * (Cfg::BX + Cfg::BW) * (128 + 16) + 2 * Cfg::BW * 4;
     static bool configured[kMaxDevices];
     if (c.device < 0 || c.device >= kMaxDevices) return hipErrorInvalidDevice;
     if (!configured[c.device]) {
