@@ -56,7 +56,8 @@ extern "C" int evomoe_test_ffn_tile(const evomoe_shape* shape, int num_cu, int64
     evomoe::Ctx c{};
     c.num_cu = num_cu;
     c.pair_hint = announced_pairs;
-    const evomoe::FfnTile t = shape->dtype == EVOMOE_BF16 ? evomoe::mfma_ffn_tile(c, *shape, kernel)
+    const bool mx8 = kernel == EVOMOE_K_FFN_MX8_GEMM1 || kernel == EVOMOE_K_FFN_MX8_GEMM2;
+    const evomoe::FfnTile t = mx8 ? evomoe::mx8_ffn_tile(c, *shape, kernel) : shape->dtype == EVOMOE_BF16 ? evomoe::mfma_ffn_tile(c, *shape, kernel)
                                                           : evomoe::f32_ffn_tile(c, *shape, kernel);
     tile[0] = t.rows; tile[1] = t.cols; tile[2] = t.waves;
     return t.rows > 0;

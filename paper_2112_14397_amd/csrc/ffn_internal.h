@@ -9,6 +9,7 @@ namespace evomoe {
 struct FfnTile { int rows, cols, waves; };
 FfnTile mfma_ffn_tile(const Ctx& c, const evomoe_shape& s, int kernel);
 FfnTile f32_ffn_tile(const Ctx& c, const evomoe_shape& s, int kernel);
+FfnTile mx8_ffn_tile(const Ctx& c, const evomoe_shape& s, int kernel);      // EVOMOE_K_FFN_MX8_GEMM1, _GEMM2
 
 // float32 matrix-core path (ffn_f32.hip)
 hipError_t f32_ffn_fwd(const Ctx& c, const evomoe_shape& s, const void* x, const int32_t* pair_token,

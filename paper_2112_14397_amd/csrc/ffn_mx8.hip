@@ -7,7 +7,7 @@
 // lanes' registers and is converted without a detour through the LDS.
 #include <type_traits>
 
-#include "kernels.h"
+#include "ffn_internal.h"
 #include "mfma_tools.h"
 #include "mx8.h"
 
@@ -28,78 +28,6 @@ struct Mx8Args {
     int E, N, K, act;
     int64_t P_cap;
 };
-
-// v_mfma_scale_f32_16x16x128_f8f6f4: lane (q = lane / 16, i = lane % 16) brings the k's 16 q .. 16 q + 15 and 64 + 16 q .. of row i
-// of either operand, and the scale of that row's k's 32 q .. 32 q + 31; it receives rows 4 q .. 4 q + 3 of column i.
-__device__ __forceinline__ f32x4 mfma16(i32x8 a, i32x8 b, f32x4 c, int sa, int sb) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, sa, 0, sb);
-}
-
-// One wave: 16 rows x 32 columns.
-template <bool FIRST>
-__global__ __launch_bounds__(64) void mx8_gemm_kernel(Mx8Args p)
-{
-    const int lane = threadIdx.x, i16 = lane & 15, q = lane >> 4;
-    int tile = blockIdx.x, g = 0, row0 = 0, rows = 0;
-    for (; g < p.E; ++g) {
-        row0 = clamp_pairs(p.expert_offsets[g], p.P_cap);
-        rows = clamp_pairs(p.expert_offsets[g + 1], p.P_cap) - row0;
-        const int n = (rows + 15) / 16;
-        if (tile < n) break;
-        tile -= n;
-    }
-    if (g == p.E) return;
-    row0 += tile * 16;
-    rows = min(16, rows - tile * 16);
-    const int r = row0 + min(i16, rows - 1), n0 = blockIdx.y * 32, kg = p.K / kMxGroup;
-    const int64_t xr = p.rows ? p.rows[r] : r;
-    const uint8_t* x = p.X + xr * p.K;
-    const uint8_t* xs = p.Xs + xr * kg;
-    const int64_t wr = (int64_t)g * p.N + n0 + i16;
-    f32x4 acc[2] = {};
-    const u32x4 zero = {};
-    for (int k = 0; k < p.K; k += 128) {
-        auto load = [&](const uint8_t* row) {
-            const int c0 = k + 16 * q, c1 = c0 + 64;
-            const u32x4 lo = c0 < p.K ? *reinterpret_cast<const u32x4*>(row + c0) : zero;
-            const u32x4 hi = c1 < p.K ? *reinterpret_cast<const u32x4*>(row + c1) : zero;
-            return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
-        };
-        auto scale = [&](const uint8_t* row) { return k / kMxGroup + q < kg ? (int)row[k / kMxGroup + q] : 127; };
-        const i32x8 b = load(x);
-        const int sb = scale(xs);
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-            acc[j] = mfma16(load(p.W + (wr + 16 * j) * p.K), b, acc[j], scale(p.Ws + (wr + 16 * j) * kg), sb);
-    }
-    // (the compiler may move a matrix instruction under the branch that uses its result, where lanes without a row would
-    // not bring their operands)
-    asm volatile("" : "+v"(acc[0]), "+v"(acc[1]));
-    float v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        v[j] = acc[j / 4][j % 4];
-        if (p.bias) v[j] += p.bias[(int64_t)g * p.N + n0 + 16 * (j / 4) + 4 * q + j % 4];
-        if (FIRST) v[j] = act_fwd(v[j], p.act);
-    }
-    if constexpr (FIRST) {
-        float m = mx_largest(v);
-        m = fmaxf(m, __shfl_xor(m, 16, 64));
-        m = fmaxf(m, __shfl_xor(m, 32, 64));
-        const uint32_t b = mx_scale_byte(m);
-        if (i16 < rows) {
-            uint8_t* out = p.Aq + (int64_t)(row0 + i16) * p.N + n0 + 4 * q;
-            *reinterpret_cast<uint32_t*>(out) = mx_pack4(v[0], v[1], v[2], v[3], b);
-            *reinterpret_cast<uint32_t*>(out + 16) = mx_pack4(v[4], v[5], v[6], v[7], b);
-            if (q == 0) p.As[(int64_t)(row0 + i16) * (p.N / kMxGroup) + n0 / kMxGroup] = (uint8_t)b;
-        }
-    } else if (i16 < rows) {
-        bf16_t* out = p.O + (int64_t)(row0 + i16) * p.N + n0 + 4 * q;
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-            *reinterpret_cast<u32x2*>(out + 16 * j) = u32x2{pack_bf16x2(v[4 * j], v[4 * j + 1]), pack_bf16x2(v[4 * j + 2], v[4 * j + 3])};
-    }
-}
 
 // gelu(h) = max(h, 0) - x 2^p(x), x = |h|: 2^p is Phi(-x), p of degree five fitted for the least largest error of the product,
 // 5e-7 with float32's own, for every finite h (p falls to -inf).  Ten VALU instructions and an exponential.
@@ -128,6 +56,104 @@ __device__ __forceinline__ void swap_halves(uint32_t& a, uint32_t& b) {
     b = v[1];
 }
 
+// EPI: what becomes of the sums.
+enum { TO_RELU = EVOMOE_RELU, TO_GELU = EVOMOE_GELU_ERF, TO_OUTPUT };
+
+// Few rows for an expert: what counts is how fast its weights arrive.  A block takes 32 rows by 32 columns and its four waves deal the
+// slabs of 128 k's among them, each straight from memory into the matrix instruction's registers, DEPTH slabs (8 loads of 1 KB each) in
+// flight; the waves' sums meet in the LDS.  K may be any multiple of 32: what lies beyond it is 0.
+template <int EPI, int DEPTH>
+__global__ __launch_bounds__(256) void mx8_few_rows_kernel(Mx8Args p)
+{
+    constexpr int LD = 33;
+    __shared__ float sums[4][32][LD];
+    const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5, wave = threadIdx.x >> 6;
+    // lane e: expert e's rows, and the row tiles up to it
+    const int begin = clamp_pairs(p.expert_offsets[min(lane, p.E)], p.P_cap),
+              end = clamp_pairs(p.expert_offsets[min(lane + 1, p.E)], p.P_cap);
+    int upto = (end - begin + 31) / 32;
+    const int mine = upto;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(upto, o, 64);
+        if (lane >= o) upto += v;
+    }
+    const int kg = p.K / kMxGroup, nct = p.N / 32;
+    const int64_t tiles = (int64_t)__builtin_amdgcn_readlane(upto, 63) * nct;
+    for (int64_t at = blockIdx.x; at < tiles; at += gridDim.x) {
+        const int tile = (int)(at / nct), n0 = (int)(at - (int64_t)tile * nct) * 32, g = __popcll(__ballot(upto <= tile));
+        const int row0 = __builtin_amdgcn_readlane(begin, g) + (tile - __builtin_amdgcn_readlane(upto - mine, g)) * 32;
+        const int rows = min(32, __builtin_amdgcn_readlane(end, g) - row0);
+        const int xr = row0 + min(l32, rows - 1);
+        const int64_t wrow = (int64_t)g * p.N + n0 + l32;
+        const uint8_t *w = p.W + wrow * p.K, *ws = p.Ws + wrow * kg;
+        const int token = p.rows ? p.rows[xr] : xr;
+        __builtin_amdgcn_sched_barrier(0);       // (the first weights are on their way before anything waits for the row number)
+        f32x16 acc = {};
+        const u32x4 zero = {};
+        for (int s0 = wave; s0 * 128 < p.K; s0 += 4 * DEPTH) {
+            u32x4 wv[DEPTH][4], xv[DEPTH][4];
+            int wsc[DEPTH][2], xsc[DEPTH][2];
+            auto load = [&](const uint8_t* row, const uint8_t* scale, u32x4 (&v)[DEPTH][4], int (&sc)[DEPTH][2]) {
+#pragma unroll
+                for (int u = 0; u < DEPTH; ++u)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int k = (s0 + 4 * u) * 128 + c * 32 + half * 16;
+                        v[u][c] = k < p.K ? *reinterpret_cast<const u32x4*>(row + k) : zero;
+                    }
+#pragma unroll
+                for (int u = 0; u < DEPTH; ++u)
+#pragma unroll
+                    for (int ks = 0; ks < 2; ++ks) {
+                        const int i = (s0 + 4 * u) * 4 + 2 * ks + half;
+                        sc[u][ks] = i < kg ? scale[i] : 127;
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            load(w, ws, wv, wsc);
+            load(p.X + (int64_t)token * p.K, p.Xs + (int64_t)token * kg, xv, xsc);
+#pragma unroll
+            for (int u = 0; u < DEPTH; ++u)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) {
+                    auto eight = [](u32x4 lo, u32x4 hi) {
+                        return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+                    };
+                    acc = mfma32<0>(eight(wv[u][2 * ks], wv[u][2 * ks + 1]), eight(xv[u][2 * ks], xv[u][2 * ks + 1]), acc, wsc[u][ks], xsc[u][ks]);
+                }
+        }
+        asm volatile("" : "+v"(acc));       // (not to be moved under a branch: see the tile kernel's epilogue)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sums[wave][8 * (r >> 2) + 4 * half + (r & 3)][l32] = acc[r];
+        __syncthreads();
+        // eight threads to a row, four columns each; the waves' sums in wave order
+        const int row = threadIdx.x >> 3, n4 = (threadIdx.x & 7) * 4;
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[j] = ((sums[0][n4 + j][row] + sums[1][n4 + j][row]) + sums[2][n4 + j][row]) + sums[3][n4 + j][row];
+            if (p.bias) v[j] += p.bias[(int64_t)g * p.N + n0 + n4 + j];
+            if (EPI == TO_RELU) v[j] = relu(v[j]);
+            if (EPI == TO_GELU) v[j] = gelu5(v[j]);
+        }
+        if constexpr (EPI == TO_OUTPUT) {
+            if (row < rows)
+                *reinterpret_cast<u32x2*>(p.O + (int64_t)(row0 + row) * p.N + n0 + n4) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        } else {
+            float m = mx_max(v);
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+            const uint32_t b = mx_scale_byte(m);
+            if (row < rows) {
+                *reinterpret_cast<uint32_t*>(p.Aq + (int64_t)(row0 + row) * p.N + n0 + n4) = mx_pack4(v[0], v[1], v[2], v[3], b);
+                if (n4 == 0) p.As[(int64_t)(row0 + row) * (p.N / kMxGroup) + n0 / kMxGroup] = (uint8_t)b;
+            }
+        }
+        __syncthreads();         // (the sums have been read)
+    }
+}
+
 // The tile kernel, for d and F that are multiples of 128.  A block of WX x WW waves computes BX rows of X by BW rows of W, a
 // wave TX x TW matrix instructions of 32 x 32.  The contraction runs in slabs of 128 bytes (one line of every row), two LDS stages
 // deep; a stage holds both operands' slabs, rows of 128 bytes with the 16-byte chunk c of row r at chunk c ^ (r >> 1 & 7), so that
@@ -137,18 +163,17 @@ __device__ __forceinline__ void swap_halves(uint32_t& a, uint32_t& b) {
 // Slab s + 2 is fetched into slab s's stage as soon as its last fragments are in registers, and lands while one and a half
 // slabs multiply.  Blocks are persistent and walk the tiles as the bf16 kernels do: expert by expert, column group by column
 // group, row tile by row tile, every XCD on a run of its own.
-// EPI: what becomes of the sums.
-enum { TO_RELU = EVOMOE_RELU, TO_GELU = EVOMOE_GELU_ERF, TO_OUTPUT };
-template <int EPI, int BX, int BW, int WX, int WW, int WPE>
+template <int EPI, int BX, int BW, int WX, int WW, int NST, int WPE>
 __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, int col_group)
 {
     constexpr bool FIRST = EPI != TO_OUTPUT;
     constexpr int NW = WX * WW, TX = BX / WX / 32, TW = BW / WW / 32;
     constexpr int XLD = BX / 8 / NW, WLD = BW / 8 / NW;         // 1 KB load instructions per wave and slab
-    constexpr int ROWS = BX + BW, SLD = ROWS / 64 / NW;         // scale load instructions per wave (64 rows each)
+    constexpr int ROWS = BX + BW, SLD = (ROWS / 64 + NW - 1) / NW;       // scale load instructions per wave (64 rows each)
     constexpr int STAGE = ROWS * 128, SCALES = ROWS * 16;
     static_assert(TW == 2 || TW == 4, "a row's scale bytes of a wave leave together");
-    static_assert(XLD * 8 * NW == BX && WLD * 8 * NW == BW && SLD * 64 * NW == ROWS && BX % 64 == 0, "whole instructions");
+    static_assert(XLD * 8 * NW == BX && WLD * 8 * NW == BW && BX % 64 == 0 && BW % 64 == 0, "whole instructions");
+    static_assert(NST >= 2 && NST <= 4, "two sets of scales hold");
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ int offs[65], tstart[65];
 
@@ -184,6 +209,8 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
         step = gridDim.x;
     }
 
+    // the 64 rows (X's, then W's) that scale load instruction i of this wave brings; instructions beyond the last repeat one
+    auto scale_rows = [&](int i) { return (wave + NW * i) % (ROWS / 64) * 64; };
     // What depends on the lane is made again for every tile's parts from a copy of the lane number that the compiler cannot see through:
     // the values then do not occupy registers through the parts that do not use them.
     auto fresh_lane = [&] { int v = lane; asm volatile("" : "+v"(v)); return v; };
@@ -207,7 +234,7 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
         const int lane = fresh_lane();
 #pragma unroll
         for (int i = 0; i < XLD + SLD; ++i)
-            xr[i] = (uint32_t)min(i < XLD ? (wave + NW * i) * 8 + (lane >> 3) : (wave + NW * (i - XLD)) * 64 + lane, t.rows - 1);
+            xr[i] = (uint32_t)min(i < XLD ? (wave + NW * i) * 8 + (lane >> 3) : scale_rows(i - XLD) + lane, t.rows - 1);
         if (p.rows) {
             const int32_t* from = p.rows + t.row0;
 #pragma unroll
@@ -232,14 +259,14 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
         for (int i = 0; i < WLD; ++i) wo[i] = (uint32_t)min((wave + NW * i) * 8 + (lane >> 3), last) * (uint32_t)p.K + chunk;
 #pragma unroll
         for (int i = 0; i < SLD; ++i) {
-            const int r = (wave + NW * i) * 64;               // X's rows, then W's; 64 of one operand, as BX is a multiple of 64
+            const int r = scale_rows(i);
             so[i] = (r < BX ? xr[XLD + i] : (uint32_t)min(r + lane - BX, last)) * (uint32_t)kg;
         }
     };
     // load instruction number x of a slab: X's rows, then W's
     constexpr int NLD = XLD + WLD;
     auto issue_one = [&](int x, int slab) {
-        unsigned char* st = smem + (slab & 1) * STAGE;
+        unsigned char* st = smem + slab % NST * STAGE;
         if (x < XLD) {
             load_to_lds(xb + slab * 128, xo[x], st + (wave + NW * x) * 1024);
         } else {
@@ -249,13 +276,13 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
     };
     // Scales, [2][ROWS][4 slabs' 4 bytes] by the parity of the four; the last four begin where they end with the row.  A contraction of
     // fewer than four slabs has them slab by slab, [slab][ROWS].
-    unsigned char* const scales = smem + 2 * STAGE;
+    unsigned char* const scales = smem + NST * STAGE;
     const bool by_four = nslab >= 4;
     auto first_of = [&](int slab) { return min(slab & ~3, nslab - 4); };
     auto issue_scales = [&](int slab) {
 #pragma unroll
         for (int i = 0; i < SLD; ++i) {
-            const int r = (wave + NW * i) * 64;
+            const int r = scale_rows(i);
             const unsigned char* from = r < BX ? xsb : wsb;
             if (by_four) load_to_lds(from + first_of(slab) * 4, so[i], scales + (slab >> 2 & 1) * SCALES + r * 16);
             else
@@ -267,7 +294,7 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
 #pragma unroll
         for (int x = 0; x < NLD; ++x) issue_one(x, slab);
     };
-    // a tile's bias (zeros, where there is none), its first scales and its first two slabs
+    // a tile's bias (zeros, where there is none), its first scales and its first slabs
     float* const bias_lds = reinterpret_cast<float*>(scales + 2 * SCALES);    // [2][BW], by the tile's parity
     auto begin = [&](const Tile& t, int parity) {
         if (p.bias) {
@@ -276,8 +303,9 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
                               reinterpret_cast<const int*>(bias_lds + parity * BW + i));
         }
         issue_scales(0);
-        issue(0);
-        if (nslab > 1) issue(1);
+#pragma unroll
+        for (int u = 0; u < NST; ++u)
+            if (u < nslab) issue(u);
     };
 
     if (!p.bias)
@@ -293,19 +321,18 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
     }
     // a wave's stores in an epilogue, at least: they follow the next tile's first loads, and are not waited for with them
     constexpr int STORES = TX * (FIRST ? TW + 1 : 2 * TW);
-    static_assert(NLD + STORES <= 63, "vmcnt");
+    static_assert((NST - 1) * NLD + STORES <= 63, "vmcnt");
     bool first = true;
     for (int parity = 0;; parity ^= 1) {
         const int lane_t = fresh_lane(), l32 = lane_t & 31, half = lane_t >> 5, key = l32 >> 1 & 7;
-        // fragment number f (W's, then X's) of k-step ks
-        auto read_one = [&](int f, int slab, int ks, i32x8 (&fw)[TW], i32x8 (&fx)[TX]) {
-            const unsigned char* st = smem + (slab & 1) * STAGE;
-            const unsigned char* row = st + (f < TW ? BX + (ww * TW + f) * 32 + l32 : (wx * TX + f - TW) * 32 + l32) * 128;
-            const u32x4 lo = *reinterpret_cast<const u32x4*>(row + (((ks * 4 + half) ^ key) << 4));
-            const u32x4 hi = *reinterpret_cast<const u32x4*>(row + (((ks * 4 + 2 + half) ^ key) << 4));
-            (f < TW ? fw[f < TW ? f : 0] : fx[f < TW ? 0 : f - TW]) =
-                i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+        auto fragment = [&](int row, int slab, int ks) {      // of k-step ks: this lane's 32 bytes of a row of the stage
+            const unsigned char* at = smem + slab % NST * STAGE + row * 128;
+            const u32x4 lo = *reinterpret_cast<const u32x4*>(at + (((ks * 4 + half) ^ key) << 4));
+            const u32x4 hi = *reinterpret_cast<const u32x4*>(at + (((ks * 4 + 2 + half) ^ key) << 4));
+            return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
         };
+        auto w_fragment = [&](int i, int slab, int ks) { return fragment(BX + (ww * TW + i) * 32 + l32, slab, ks); };
+        auto x_fragment = [&](int j, int slab, int ks) { return fragment((wx * TX + j) * 32 + l32, slab, ks); };
         auto read_scales = [&](int slab, int (&sw)[TW], int (&sx)[TX]) {
             const int per_row = by_four ? 16 : 4;
             const unsigned char* st = scales + (by_four ? (slab >> 2 & 1) * SCALES + (slab - first_of(slab)) * 4 : slab * ROWS * 4) + l32 * per_row;
@@ -315,26 +342,26 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
             for (int j = 0; j < TX; ++j) sx[j] = *reinterpret_cast<const int*>(st + (wx * TX + j) * 32 * per_row);
         };
         f32x16 acc[TW][TX];
-        i32x8 w0[TW], x0[TX], w1[TW], x1[TX];
+        i32x8 w0[TW], w1[TW], x[TX];
         int sw[TW], sx[TX], sw_next[TW], sx_next[TX];
-        // One k-step (64 k's): its matrix instructions, and between them, pinned there, the reads of the next k-step's fragments (the
-        // first half of the instructions take them) and a later slab's loads.
-        auto kstep = [&](auto op, auto begins, const i32x8 (&fw)[TW], const i32x8 (&fx)[TX], auto&& between) {
-            constexpr int NMF = TW * TX;
+        // One k-step (64 k's) on w and x: its matrix instructions, and between them, pinned there, the reads of the next k-step's fragments
+        // (next: there is one, k-step ks of slab `slab`), W's into the other set, X's into a fragment's own registers after its last use,
+        // and what else is to go out.
+        auto kstep = [&](auto op, auto begins, auto next, const i32x8 (&w)[TW], i32x8 (&w_next)[TW], int slab, int ks, auto&& also) {
 #pragma unroll
-            for (int m = 0; m < NMF; ++m) {
-                const int j = m / TW, i = m % TW;
-                acc[i][j] = mfma32<decltype(op)::value>(fw[i], fx[j], decltype(begins)::value ? f32x16{} : acc[i][j], sw[i], sx[j]);
-                between(m, NMF);
-                __builtin_amdgcn_sched_barrier(0);
+            for (int j = 0; j < TX; ++j) {
+#pragma unroll
+                for (int i = 0; i < TW; ++i) {
+                    const int m = j * TW + i;
+                    acc[i][j] = mfma32<decltype(op)::value>(w[i], x[j], decltype(begins)::value ? f32x16{} : acc[i][j], sw[i], sx[j]);
+                    also(m);
+                    if (decltype(next)::value) {
+                        if (m < TW) w_next[m] = w_fragment(m, slab, ks);
+                        if (i == TW - 1) x[j] = x_fragment(j, slab, ks);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
-        };
-        constexpr int NFR = TW + TX;
-        auto read_share = [&](int m, int n, int slab, int ks, i32x8 (&fw)[TW], i32x8 (&fx)[TX]) {
-            const int h = n / 2;
-            if (m >= h) return;
-#pragma unroll
-            for (int f = NFR * m / h; f < NFR * (m + 1) / h; ++f) read_one(f, slab, ks, fw, fx);
         };
         auto use_scales = [&](const int (&w)[TW], const int (&x)[TX]) {       // this half's bytes: 0 (first k-step) and 2 (second)
 #pragma unroll
@@ -342,51 +369,55 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
 #pragma unroll
             for (int j = 0; j < TX; ++j) sx[j] = (int)((uint32_t)x[j] >> (8 * half));
         };
-        if (nslab == 1) wait_vmcnt<0>();
-        else if (first) wait_vmcnt<NLD>();
-        else wait_vmcnt<NLD + STORES>();
+        if (nslab < NST) wait_vmcnt<0>();
+        else if (first) wait_vmcnt<(NST - 1) * NLD>();
+        else wait_vmcnt<(NST - 1) * NLD + STORES>();
         first = false;
         block_sync_lds();
 #pragma unroll
-        for (int f = 0; f < NFR; ++f) read_one(f, 0, 0, w0, x0);
+        for (int i = 0; i < TW; ++i) w0[i] = w_fragment(i, 0, 0);
+#pragma unroll
+        for (int j = 0; j < TX; ++j) x[j] = x_fragment(j, 0, 0);
         read_scales(0, sw_next, sx_next);
         use_scales(sw_next, sx_next);
         constexpr auto OP0 = std::integral_constant<int, 0>{};
         constexpr auto OP2 = std::integral_constant<int, 2>{};
-        auto first_half = [&](int s, auto begins) {
-            kstep(OP0, begins, w0, x0, [&](int m, int n) { read_share(m, n, s, 1, w1, x1); });
-        };
-        auto second_half = [&](int s, auto more) {            // of a slab that has a next; more: which has a next as well
-            wait_vmcnt<0>();
+        constexpr auto YES = std::true_type{};
+        constexpr auto NO = std::false_type{};
+        auto first_half = [&](int s, auto begins) { kstep(OP0, begins, YES, w0, w1, s, 1, [](int) {}); };
+        auto second_half = [&](int s, auto more) {            // of a slab that has a next; more: there is a slab s + NST
+            // (of the loads that came after slab s + 1's, all may be on their way)
+            if (decltype(more)::value || s + NST == nslab) wait_vmcnt<(NST - 2) * NLD>();
+            else if (NST == 4 && s + 3 == nslab) wait_vmcnt<NLD>();
+            else wait_vmcnt<0>();
             block_sync_lds();                                 // slab s + 1 is there, and everybody has slab s in registers
-            kstep(OP2, std::false_type{}, w1, x1, [&](int m, int n) {
+            kstep(OP2, NO, YES, w1, w0, s + 1, 0, [&](int m) {
                 if (m == 0) read_scales(s + 1, sw_next, sx_next);
-                read_share(m, n, s + 1, 0, w0, x0);
                 if (decltype(more)::value) {
-                    if (m == 0 && (s + 2) % 4 == 0) issue_scales(s + 2);
+                    if (m == 0 && (s + NST) % 4 == 0) issue_scales(s + NST);
 #pragma unroll
-                    for (int x = NLD * m / n; x < NLD * (m + 1) / n; ++x) issue_one(x, s + 2);
+                    for (int u = NLD * m / (TX * TW); u < NLD * (m + 1) / (TX * TW); ++u) issue_one(u, s + NST);
                 }
             });
             use_scales(sw_next, sx_next);
         };
-        first_half(0, std::true_type{});
+        first_half(0, YES);
         int s = 0;
-        for (; s + 2 < nslab; ++s) {
-            second_half(s, std::true_type{});
-            first_half(s + 1, std::false_type{});
+        for (; s + NST < nslab; ++s) {
+            second_half(s, YES);
+            first_half(s + 1, NO);
         }
         // the next tile's row numbers arrive under the last slabs
         const bool more_tiles = seq + step < seq_end;
         Tile next = t;
         if (more_tiles) next = locate(seq + step);
-        if (s + 1 < nslab) {
-            second_half(s, std::false_type{});
-            first_half(s + 1, std::false_type{});
+        for (; s + 1 < nslab; ++s) {
+            second_half(s, NO);
+            first_half(s + 1, NO);
         }
         uint32_t xr[XLD + SLD];
         x_rows(next, xr);
-        kstep(OP2, std::false_type{}, w1, x1, [&](int, int) {});
+        kstep(OP2, NO, NO, w1, w0, 0, 0, [](int) {});
         // (the compiler would move these matrix instructions down to where their sums are read, and keep their operands until there)
         auto pin = [](f32x16& sums) {
             if constexpr (TW * TX * 16 > 128) asm volatile("" : "+a"(sums));
@@ -407,31 +438,30 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
         // instruction whose result only some lanes use may be moved under their branch, where the others bring no operands) ----
         {
             const int lane_e = fresh_lane(), l32 = lane_e & 31, half = lane_e >> 5;
+            uint32_t bytes[TX][TW];
 #pragma unroll
-            for (int j = 0; j < TX; ++j) {
-                const int r0 = (wx * TX + j) * 32, there = min(32, max(0, t.rows - r0));
-                const int64_t at = (int64_t)(t.row0 + r0);
-                uint32_t bytes[TW];
+            for (int i = 0; i < TW; ++i) {
+                const int n = t.n0 + (ww * TW + i) * 32;      // N is a multiple of 32
+                const uint32_t beyond = n < p.N ? 0u : 0x40000000u;
+                f32x4 bias[4];
 #pragma unroll
-                for (int i = 0; i < TW; ++i) {
-                    const int n = t.n0 + (ww * TW + i) * 32;  // N is a multiple of 32
-                    const uint32_t beyond = n < p.N ? 0u : 0x40000000u;
+                for (int q = 0; q < 4; ++q)
+                    bias[q] = *reinterpret_cast<const f32x4*>(bias_lds + parity * BW + (ww * TW + i) * 32 + 8 * q + 4 * half);
+#pragma unroll
+                for (int j = 0; j < TX; ++j) {
+                    const int r0 = (wx * TX + j) * 32, there = min(32, max(0, t.rows - r0));
+                    const int64_t at = (int64_t)(t.row0 + r0);
                     pin(acc[i][j]);                           // (one unit's sums in vector registers at a time)
                     float v[16];
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) v[r] = acc[i][j][r];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const f32x4 b = *reinterpret_cast<const f32x4*>(bias_lds + parity * BW + (ww * TW + i) * 32 + 8 * q + 4 * half);
-                        v[4 * q] += b.x; v[4 * q + 1] += b.y; v[4 * q + 2] += b.z; v[4 * q + 3] += b.w;
-                    }
+                    for (int r = 0; r < 16; ++r) v[r] = acc[i][j][r] + bias[r / 4][r % 4];
                     if constexpr (FIRST) {
 #pragma unroll
                         for (int r = 0; r < 16; ++r) v[r] = EPI == TO_RELU ? relu(v[r]) : gelu5(v[r]);
                         uint32_t ma = __float_as_uint(mx_max(v)), mb = ma;      // (of a group with an infinity any scale will do: O is NaN)
                         swap_halves(ma, mb);
                         const uint32_t b = mx_scale_byte(fmaxf(__uint_as_float(ma), __uint_as_float(mb)));
-                        bytes[i] = b;
+                        bytes[j][i] = b;
                         uint32_t d[4];
 #pragma unroll
                         for (int q = 0; q < 4; ++q) d[q] = mx_pack4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3], b);
@@ -451,14 +481,18 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                if constexpr (FIRST) {
-                    const int ng = p.N / kMxGroup, n = (t.n0 + ww * TW * 32) / kMxGroup;
-                    const auto to = rows_of(p.As + at * ng, there * ng);
-                    const int off = half || n >= ng ? 0x40000000 : l32 * ng + n;       // (N is a multiple of a wave's columns)
+            }
+            if constexpr (FIRST) {
+                const int ng = p.N / kMxGroup, n = (t.n0 + ww * TW * 32) / kMxGroup;
+                const int off = half || n >= ng ? 0x40000000 : l32 * ng + n;           // (N is a multiple of a wave's columns)
+#pragma unroll
+                for (int j = 0; j < TX; ++j) {
+                    const int r0 = (wx * TX + j) * 32, there = min(32, max(0, t.rows - r0));
+                    const auto to = rows_of(p.As + (int64_t)(t.row0 + r0) * ng, there * ng);
                     if constexpr (TW == 4)
-                        __builtin_amdgcn_raw_buffer_store_b32(bytes[0] | bytes[1] << 8 | bytes[2 % TW] << 16 | bytes[3 % TW] << 24, to, off, 0, 0);
+                        __builtin_amdgcn_raw_buffer_store_b32(bytes[j][0] | bytes[j][1] << 8 | bytes[j][2 % TW] << 16 | bytes[j][3 % TW] << 24, to, off, 0, 0);
                     else
-                        __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(bytes[0] | bytes[1] << 8), to, off, 0, 0);
+                        __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(bytes[j][0] | bytes[j][1] << 8), to, off, 0, 0);
                 }
             }
         }
@@ -468,18 +502,41 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
     }
 }
 
-template <bool FIRST> hipError_t launch_small(const Ctx& c, const evomoe_shape& s, const Mx8Args& a) {
-    const dim3 grid((unsigned)((s.P_cap + 15) / 16 + s.E), (unsigned)(a.N / 32));
-    hipLaunchKernelGGL(mx8_gemm_kernel<FIRST>, grid, dim3(64), 0, c.stream, a);
-    return hipGetLastError();
+// Tiles.  BIG: one block per compute unit, four waves of 128x128; the least LDS traffic per product.  BIG8: the same tile by eight waves
+// (128x64 each, two to a SIMD): they fill each other's stalls in an epilogue that gelu and conversion make as long as the main loop.
+// MID: 128x128, two blocks per unit, one's epilogue under the other's products.  DEEP: 128x128 with four slabs on their way, for
+// long contractions with few tiles.  SML: 64x128.  us, E = 16, d = 768, F = 3072 (but for the last row) / E = 64, d = 1024, F = 4096:
+//   first product, pairs   48   512  2048  5998 16384 65536 /    96 65536    second product   48   512  2048  5998 16384 65536 / 65536
+//     SML                 13.0  14.4  20.6  40.6  96.2   359 /  48.5   575                   20.4  21.0  22.9  44.6  79.1   315 /   542
+//     MID                 14.8  16.2  21.9  37.0  79.9   281 /  52.6   467                   20.8  21.7  24.4  47.6  60.9   230 /   391
+//     DEEP                20.0  20.3  27.7  44.2   104   381 /  66.9   561                   16.7  17.2  20.5  36.7  67.1   244 /   416
+//     BIG                   -   23.4  25.1  44.0  84.1   276 /    -    445                     -   36.2  38.1  42.8  49.6   207 /   325
+//     BIG8                  -   21.8  23.9  40.8  77.2   256 /    -    420                     -   35.3  37.8  42.2  50.5   218 /   342
+//     few rows            16.4  25.1  62.9   157     -     - /  74.5     -                   17.9  28.1  65.9   162     -     - /     -
+// Few rows where no more than a pair falls to an expert and their weights are little (8 tokens, 16 pairs: 20 us for both, in tiles 29;
+// one token 13, 23), and for sizes that the tile kernel does not take.
+struct Big { static constexpr int BX = 256, BW = 256, WX = 2, WW = 2, NST = 2, WPE = 1, BLOCKS = 1; };
+struct Big8 { static constexpr int BX = 256, BW = 256, WX = 2, WW = 4, NST = 2, WPE = 2, BLOCKS = 1; };
+struct Mid { static constexpr int BX = 128, BW = 128, WX = 2, WW = 2, NST = 2, WPE = 2, BLOCKS = 2; };
+struct Deep { static constexpr int BX = 128, BW = 128, WX = 2, WW = 2, NST = 4, WPE = 1, BLOCKS = 1; };
+struct Sml { static constexpr int BX = 64, BW = 128, WX = 2, WW = 2, NST = 2, WPE = 2, BLOCKS = 2; };
+
+enum class Pick { FewRows, Sml, Mid, Deep, Big, Big8 };
+Pick pick(const Ctx& c, const evomoe_shape& s, bool first) {
+    const int64_t pairs = c.pair_hint > 0 && c.pair_hint < s.P_cap ? c.pair_hint : s.P_cap, weights = (int64_t)s.d * s.F;
+    if (s.d % 128 || s.F % 128 || (pairs <= s.E && pairs * weights <= 40000000)) return Pick::FewRows;
+    // 256x256 tiles: an expert fills two of them, and there are enough (short contractions need more, their epilogues being long)
+    const int n = first ? s.F : s.d;
+    const int64_t tiles = ((pairs + 255) / 256 + s.E / 2) * ((n + 255) / 256);
+    if (pairs >= 512 * s.E && tiles >= (first ? 2 * c.num_cu : c.num_cu / 2)) return first ? Pick::Big8 : Pick::Big;
+    if (!first) return Pick::Deep;
+    return pairs >= 256 * s.E ? Pick::Mid : Pick::Sml;
 }
 
-struct Big { static constexpr int BX = 256, BW = 256, WX = 2, WW = 2, WPE = 1; };
-struct Mid { static constexpr int BX = 128, BW = 128, WX = 2, WW = 2, WPE = 2; };
-
 template <int EPI, class Cfg> hipError_t launch_tiles(const Ctx& c, const evomoe_shape& s, const Mx8Args& a) {
-    auto kern = mx8_tile_kernel<EPI, Cfg::BX, Cfg::BW, Cfg::WX, Cfg::WW, Cfg::WPE>;
-    constexpr int smem = 2 * (Cfg::BX + Cfg::BW) * (128 + 16) + 2 * Cfg::BW * 4;
+    auto kern = mx8_tile_kernel<EPI, Cfg::BX, Cfg::BW, Cfg::WX, Cfg::WW, Cfg::NST, Cfg::WPE>;
+    constexpr int smem = (Cfg::BX + Cfg::BW) * (Cfg::NST * 128 + 2 * 16) + 2 * Cfg::BW * 4;
+    static_assert((smem + 1024) * Cfg::BLOCKS <= 160 * 1024, "LDS");
     static bool configured[kMaxDevices];
     if (c.device < 0 || c.device >= kMaxDevices) return hipErrorInvalidDevice;
     if (!configured[c.device]) {
@@ -488,28 +545,53 @@ template <int EPI, class Cfg> hipError_t launch_tiles(const Ctx& c, const evomoe
         configured[c.device] = true;
     }
     const int nct = (a.N + Cfg::BW - 1) / Cfg::BW;
-    const int64_t worst = ((s.P_cap + Cfg::BX - 1) / Cfg::BX + s.E) * nct, cap = (int64_t)c.num_cu * Cfg::WPE;
+    const int64_t worst = ((s.P_cap + Cfg::BX - 1) / Cfg::BX + s.E) * nct, cap = (int64_t)c.num_cu * Cfg::BLOCKS;
+    // column tiles whose weight panels stay in an XCD's L2 together, or all where a row panel is as large itself
     const int64_t fit = (int64_t)(2.4 * 1024 * 1024) / ((int64_t)Cfg::BW * a.K);
     const int col_group = (int64_t)Cfg::BX * a.K >= (1 << 20) ? nct : (int)(fit < 1 ? 1 : fit > nct ? nct : fit);
     hipLaunchKernelGGL(kern, dim3((unsigned)(worst < cap ? worst : cap)), dim3(Cfg::WX * Cfg::WW * 64), smem, c.stream, a, col_group);
     return hipGetLastError();
 }
 
-template <bool FIRST> hipError_t launch(const Ctx& c, const evomoe_shape& s, const Mx8Args& a) {
-    const int64_t pairs = c.pair_hint > 0 && c.pair_hint < s.P_cap ? c.pair_hint : s.P_cap;
-    if (s.d % 128 || s.F % 128 || pairs < 32 * s.E) return launch_small<FIRST>(c, s, a);
-    const int64_t tiles = ((pairs + 255) / 256 + s.E / 2) * ((a.N + 255) / 256);
-    auto run = [&](auto epi) {
-        constexpr int EPI = decltype(epi)::value;
-        return tiles >= 2 * c.num_cu ? launch_tiles<EPI, Big>(c, s, a) : launch_tiles<EPI, Mid>(c, s, a);
-    };
-    if (!FIRST) return run(std::integral_constant<int, TO_OUTPUT>{});
-    return a.act == EVOMOE_RELU ? run(std::integral_constant<int, TO_RELU>{}) : run(std::integral_constant<int, TO_GELU>{});
+template <int EPI> hipError_t launch_few_rows(const Ctx& c, const evomoe_shape& s, const Mx8Args& a) {
+    const int64_t worst = ((s.P_cap + 31) / 32 + s.E) * (a.N / 32), cap = (int64_t)c.num_cu * 16;
+    const dim3 grid((unsigned)(worst < cap ? worst : cap));
+    if (a.K <= 1024) hipLaunchKernelGGL((mx8_few_rows_kernel<EPI, 2>), grid, dim3(256), 0, c.stream, a);
+    else hipLaunchKernelGGL((mx8_few_rows_kernel<EPI, 3>), grid, dim3(256), 0, c.stream, a);
+    return hipGetLastError();
+}
+
+template <int EPI> hipError_t launch_first(const Ctx& c, const evomoe_shape& s, const Mx8Args& a) {
+    switch (pick(c, s, true)) {
+        case Pick::FewRows: return launch_few_rows<EPI>(c, s, a);
+        case Pick::Sml: return launch_tiles<EPI, Sml>(c, s, a);
+        case Pick::Mid: return launch_tiles<EPI, Mid>(c, s, a);
+        default: return launch_tiles<EPI, Big8>(c, s, a);
+    }
+}
+hipError_t launch_second(const Ctx& c, const evomoe_shape& s, const Mx8Args& a) {
+    switch (pick(c, s, false)) {
+        case Pick::FewRows: return launch_few_rows<TO_OUTPUT>(c, s, a);
+        case Pick::Deep: return launch_tiles<TO_OUTPUT, Deep>(c, s, a);
+        default: return launch_tiles<TO_OUTPUT, Big>(c, s, a);
+    }
 }
 
 size_t aq_bytes(const evomoe_shape& s) { return ((size_t)s.P_cap * s.F + 255) & ~(size_t)255; }
 
 }  // namespace
+
+FfnTile mx8_ffn_tile(const Ctx& c, const evomoe_shape& s, int kernel) {
+    switch (pick(c, s, kernel == EVOMOE_K_FFN_MX8_GEMM1)) {
+        case Pick::FewRows: return {32, 32, 4};
+        case Pick::Sml: return {Sml::BX, Sml::BW, 4};
+        case Pick::Mid: return {Mid::BX, Mid::BW, 4};
+        case Pick::Deep: return {Deep::BX, Deep::BW, 4};
+        case Pick::Big: return {Big::BX, Big::BW, 4};
+        case Pick::Big8: return {Big8::BX, Big8::BW, 8};
+    }
+    return {};
+}
 
 // [A : P_cap x F bytes, rounded up to 256][its scales]
 size_t ffn_mx8_workspace_bytes(const evomoe_shape& s) {
@@ -527,13 +609,13 @@ hipError_t launch_expert_ffn_mx8(const Ctx& c, const evomoe_shape& s, const void
     hipError_t err;
     {
         ProfScope ps(c, EVOMOE_K_FFN_MX8_GEMM1);
-        err = launch<true>(c, s, a);
+        err = s.act == EVOMOE_RELU ? launch_first<TO_RELU>(c, s, a) : launch_first<TO_GELU>(c, s, a);
     }
     if (err != hipSuccess) return err;
     a.X = Aq; a.Xs = As; a.W = (const uint8_t*)W2_q; a.Ws = W2_scale; a.rows = nullptr; a.bias = b2; a.O = (bf16_t*)O;
     a.N = s.d; a.K = s.F;
     ProfScope ps(c, EVOMOE_K_FFN_MX8_GEMM2);
-    return launch<false>(c, s, a);
+    return launch_second(c, s, a);
 }
 
 }  // namespace evomoe

@@ -52,7 +52,18 @@ def run(ctx, values, offsets, token, b1, b2, act, P_cap, T, gather=True):
     return O
 
 
-def check(ctx, T, d, E, F, P, act, seed=0, biases=True, gather=True, room=0, hint=0):
+def some_rows(offsets, rng):
+    """Rows that are compared where comparing all takes too long: the first and last ones of every expert, those around multiples of
+    the tiles' 32 to 256 rows, and others."""
+    rows = set(rng.integers(0, int(offsets[-1]), 60).tolist())
+    for a, b in zip(offsets[:-1].tolist(), offsets[1:].tolist()):
+        for r in (a, a + 1, a + 31, a + 32, a + 63, a + 64, a + 127, a + 128, a + 255, a + 256, b - 129, b - 2, b - 1):
+            if a <= r < b:
+                rows.add(r)
+    return np.array(sorted(rows))
+
+
+def check(ctx, T, d, E, F, P, act, seed=0, biases=True, gather=True, room=0, hint=0, some=False):
     rng = np.random.default_rng(seed + T + d + E + F)
     values, offsets, token, b1, b2 = inputs(rng, T if gather else P, d, E, F, P)
     if not biases:
@@ -65,10 +76,13 @@ def check(ctx, T, d, E, F, P, act, seed=0, biases=True, gather=True, room=0, hin
     assert torch.equal(O, again)
     assert (O[P:] == 7).all()                                     # rows behind the last pair are left as they were
     x, W1, W2 = (blk.mx8_value(*values[n]) for n in ("x", "W1", "W2"))
+    rows = some_rows(offsets, rng) if some else np.arange(P)
+    if not gather:
+        token = np.arange(P)
     # sums over max(d, F) products of 8-bit values and scales, which are exact: one rounding each (two steps of slack for the
     # matrix instruction, which may cut off instead of rounding)
-    want, bound = blk.experts_mx8(x, token if gather else None, offsets, W1, b1, W2, b2, act, 2 * U * max(d, F), ACT)
-    got = O[:P].double().cpu().numpy()
+    want, bound = blk.experts_mx8(x, token[rows], np.searchsorted(rows, offsets), W1, b1, W2, b2, act, 2 * U * max(d, F), ACT)
+    got = O[:P].double().cpu().numpy()[rows]
     bad = ~(abs(got - want) <= bound + 2.0 ** -8 * abs(want))
     assert not bad.any(), (int(bad.sum()), got[bad][:4], want[bad][:4], bound[bad][:4])
 
@@ -80,14 +94,37 @@ def ctx():
     c.close()
 
 
-CASES = [(1, 32, 1, 32, 1), (5, 64, 3, 96, 9), (48, 768, 16, 1024, 48), (70, 160, 7, 288, 200), (300, 256, 4, 512, 700),
-         (40, 1056, 5, 64, 90), (90, 96, 64, 128, 400), (600, 128, 2, 256, 1500), (33, 512, 33, 544, 33)]
+# T, d, E, F, pairs, and the tiles of both products
+CASES = [(1, 32, 1, 32, 1, "32x32/4", "32x32/4"), (5, 64, 3, 96, 9, "32x32/4", "32x32/4"), (48, 768, 16, 1024, 16, "32x32/4", "32x32/4"),
+         (70, 160, 7, 288, 200, "32x32/4", "32x32/4"), (40, 1056, 5, 64, 90, "32x32/4", "32x32/4"),
+         (33, 512, 33, 544, 33, "32x32/4", "32x32/4"), (300, 1184, 2, 32, 400, "32x32/4", "32x32/4"),
+         (48, 768, 16, 1024, 48, "64x128/4", "128x128/4"), (300, 256, 4, 512, 700, "64x128/4", "128x128/4"),
+         (90, 128, 64, 128, 400, "64x128/4", "128x128/4"), (60, 384, 5, 640, 77, "64x128/4", "128x128/4"),
+         (600, 128, 2, 256, 1500, "128x128/4", "128x128/4"), (500, 640, 3, 384, 1100, "128x128/4", "128x128/4"),
+         (100, 512, 1, 1152, 333, "128x128/4", "128x128/4")]
+# ... where the oracle looks at some rows
+LARGE = [(500, 128, 2, 4352, 8100, "256x256/8", "128x128/4"), (400, 384, 1, 8832, 4000, "256x256/8", "128x128/4"),
+         (700, 1024, 3, 128, 8200, "128x128/4", "256x256/4"), (300, 4480, 2, 256, 2600, "128x128/4", "256x256/4"),
+         (900, 1152, 5, 4736, 9000, "256x256/8", "256x256/4")]
 
 
-@pytest.mark.parametrize("T,d,E,F,P", CASES)
+@pytest.mark.parametrize("T,d,E,F,P,first,second", CASES)
 @pytest.mark.parametrize("act", ["gelu", "relu"])
-def test_against_the_oracle(ctx, T, d, E, F, P, act):
-    check(ctx, T, d, E, F, P, act, biases=act == "gelu", room=37)
+def test_against_the_oracle(ctx, T, d, E, F, P, first, second, act):
+    check(ctx, T, d, E, F, P, act, biases=act == "gelu", room=37, hint=P)
+
+
+@pytest.mark.parametrize("T,d,E,F,P,first,second", LARGE)
+def test_large_tiles(ctx, T, d, E, F, P, first, second):
+    check(ctx, T, d, E, F, P, "gelu", room=300, hint=P, some=True)
+    if d == 128:
+        check(ctx, T, d, E, F, P, "relu", biases=False, some=True)
+
+
+def test_a_hint_that_is_wrong(ctx):
+    """An announced pair count picks the tiles and nothing else: far too few, far too many."""
+    check(ctx, 300, 256, 4, 512, 700, "gelu", hint=1)
+    check(ctx, 60, 256, 4, 512, 31, "gelu", room=40000, hint=40000)
 
 
 def test_rows_that_are_permuted_already(ctx):
