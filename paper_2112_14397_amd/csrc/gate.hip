@@ -991,13 +991,6 @@ hipError_t launch_dts_gate_bwd(const Ctx& c, const evomoe_shape& s, const float*
     return launch_gate_logits_bwd(c, s, dz, x, Wg, dx, dWg, dbg, dx, dz + (size_t)s.T * s.E);
 }
 
-// out[i] = sum of rows of part [n_rows][n], i < n
-hipError_t launch_sum_rows(const Ctx& c, const float* part, int n_rows, size_t n, float* out) {
-    hipLaunchKernelGGL(sum_chunks_kernel, dim3((n + 63) / 64), dim3(256), 0, c.stream, part, n_rows, n, (size_t)0, out,
-                       (float*)nullptr);
-    return hipGetLastError();
-}
-
 // ---------------------------------------------------------------------------------------------
 // Balance loss (Eq. balance_loss): L = alpha N sum_i (count_i / T^2) sum_s g'_si and dL/dg'_si.
 // Pass 1: per-block column sums of g' (thread = (token lane, expert), fixed-order LDS reduction over the

@@ -22,7 +22,6 @@ hipError_t launch_gate_logits_bwd(const Ctx& c, const evomoe_shape& s, const flo
                                   const void* dx_in, float* dWg, float* dbg, void* dx, float* part);
 // clears counts [E] and block_hist (may be null)
 hipError_t launch_clear_counts(const Ctx& c, const evomoe_shape& s, int32_t* counts, int32_t* block_hist);
-hipError_t launch_sum_rows(const Ctx& c, const float* part, int n_rows, size_t n, float* out);
 // balance loss: scratch holds balance_blocks(s) * E floats of per-block column sums of g'
 int balance_blocks(const evomoe_shape& s);
 hipError_t launch_balance_loss(const Ctx& c, const evomoe_shape& s, const float* gprime, const int32_t* counts,
