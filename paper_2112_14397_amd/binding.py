@@ -127,7 +127,7 @@ def _p(t: Optional[torch.Tensor]):
     if t is None:
         return None
     assert t.is_cuda and t.is_contiguous(), "device, contiguous tensors only"
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()                       # (an int: the calls' argument types make a pointer of it)
 
 
 def _chk(st: int, where: str):
