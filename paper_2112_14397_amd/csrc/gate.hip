@@ -460,6 +460,77 @@ hipError_t launch_dts_gate(const Ctx& c, const evomoe_shape& s, const void* x, c
                                  counts, k_per_token, block_hist);
 }
 
+// Logits alone of a bf16 layer's few tokens: one launch, in which 16 waves share the k-blocks of 16 tokens and split W_g themselves, as
+// reading it 16 at a time costs less than a second launch.
+template <int NE>
+__global__ __launch_bounds__(1024) void logits_few_kernel(const bf16_t* __restrict__ x, const float* __restrict__ Wg,
+                                                          const float* __restrict__ bg, int T, int d, int E, float* __restrict__ logits)
+{
+    constexpr int LDZ = 16 * NE, XU = 2;                     // k-blocks of a wave whose loads are on their way together
+    __shared__ float part[16][16 * LDZ];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i16 = lane & 15, q = lane >> 4;
+    const int t0 = blockIdx.x * 16, t = t0 + i16;
+    f32x4 acc[NE];
+#pragma unroll
+    for (int n = 0; n < NE; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int kb = wave; kb * 32 < d; kb += 16 * XU) {
+        bf16x8 a[XU];
+        float w[XU][NE][8];
+#pragma unroll
+        for (int u = 0; u < XU; ++u) {
+            const int k0 = (kb + 16 * u) * 32 + q * 8;       // (d is a multiple of 8)
+            a[u] = k0 < d && t < T ? *reinterpret_cast<const bf16x8*>(x + (size_t)t * d + k0) : bf16x8{};
+#pragma unroll
+            for (int n = 0; n < NE; ++n)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    w[u][n][j] = k0 < d && n * 16 + i16 < E ? Wg[(size_t)(k0 + j) * E + n * 16 + i16] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < XU; ++u)
+#pragma unroll
+            for (int n = 0; n < NE; ++n) {
+                bf16x8 hi, mid, lo;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    hi[j] = (bf16_t)w[u][n][j];
+                    const float r1 = w[u][n][j] - (float)hi[j];
+                    mid[j] = (bf16_t)r1;
+                    lo[j] = (bf16_t)(r1 - (float)mid[j]);
+                }
+                acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[u], lo, acc[n], 0, 0, 0);
+                acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[u], mid, acc[n], 0, 0, 0);
+                acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[u], hi, acc[n], 0, 0, 0);
+            }
+    }
+#pragma unroll
+    for (int n = 0; n < NE; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) part[wave][(4 * q + r) * LDZ + n * 16 + i16] = acc[n][r];
+    __syncthreads();
+    const int n = min(16, T - t0) * E;
+    for (int i = threadIdx.x; i < n; i += 1024) {
+        const int tl = i / E, e = i - tl * E;
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) sum += part[w][tl * LDZ + e];
+        logits[(size_t)t0 * E + i] = sum + (bg ? bg[e] : 0.f);
+    }
+}
+// Whose blocks, one to 16 tokens, take no more than one trip over the CUs and for many experts less, as every block splits all of W_g
+// (us a call, one launch / two: T = 48, d = 768, E = 16 4.4 / 7.4, T = 4096 4.5 / 7.6; T = 256, d = 1024, E = 64 9.9 / 10.6, T = 1024
+// 10.6 / 10.5, T = 4096 14.1 / 11.9; T = 16384, d = 768, E = 32 19.9 / 13.5).
+static bool few_logits(const Ctx& c, const evomoe_shape& s) {
+    return s.dtype == EVOMOE_BF16 && (int64_t)s.T * ((s.E + 15) / 16) <= 16 * c.num_cu;
+}
+template <int NE>
+static hipError_t logits_few_launch(const Ctx& c, const evomoe_shape& s, const void* x, const float* Wg, const float* bg, float* logits) {
+    ProfScope ps(c, EVOMOE_K_GATE_LOGITS);
+    hipLaunchKernelGGL(logits_few_kernel<NE>, dim3((s.T + 15) / 16), dim3(1024), 0, c.stream, (const bf16_t*)x, Wg, bg, s.T, s.d, s.E,
+                       logits);
+    return hipGetLastError();
+}
+
 template <typename TX, int NE, int RT>
 static hipError_t logits_launch_t(const Ctx& c, const evomoe_shape& s, const void* x, const float* Wg, const float* bg,
                                   float* logits) {
@@ -485,6 +556,7 @@ static hipError_t logits_launch(const Ctx& c, const evomoe_shape& s, const void*
     const int rt = pick_rt(c, s);
     auto with = [&](auto ne) {
         constexpr int NE = decltype(ne)::value;
+        if (few_logits(c, s)) return logits_few_launch<NE>(c, s, x, Wg, bg, logits);
         return rt == 4 ? logits_launch_t<TX, NE, 4>(c, s, x, Wg, bg, logits)
              : rt == 2 ? logits_launch_t<TX, NE, 2>(c, s, x, Wg, bg, logits)
                        : logits_launch_t<TX, NE, 1>(c, s, x, Wg, bg, logits);

@@ -287,7 +287,8 @@ __global__ __launch_bounds__(kTopkThreads<LPT>) void topk_gate_kernel(TopkArgs a
     float bias[4], z_next[4];
     load4(a.bias, a.bias != nullptr, 0, e0, E, 0.f, bias);
     load4(a.logits, t0 + tl < t1, (size_t)(t0 + tl) * E, e0, E, -INFINITY, z_next);
-    for (int t = t0 + tl; t - tl < t1; t += TPB) {
+    // (a wave ends with its own last token)
+    for (int t = t0 + tl, first = __builtin_amdgcn_readfirstlane(t); first < t1; t += TPB, first += TPB) {
         const bool there = t < t1;
         const size_t at = (size_t)t * E;
         float z[4], s[4], rest[4], key[4];
