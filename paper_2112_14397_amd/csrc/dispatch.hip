@@ -84,10 +84,18 @@ __global__ __launch_bounds__(256) void dispatch_scatter_kernel(
         const int e = tid % EP, rl = tid / EP;
         int p = 0, a = 0;
         if (e < E)
-            for (int b = rl; b < nblk; b += 256 / EP) {
-                const int v = block_counts[(size_t)b * E + e];
-                a += v;
-                if (b < (int)blockIdx.x) p += v;
+            for (int b0 = rl; b0 < nblk; b0 += 8 * (256 / EP)) {       // (eight rows on their way together)
+                int v[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int b = b0 + u * (256 / EP);
+                    v[u] = b < nblk ? block_counts[(size_t)b * E + e] : 0;
+                }
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    a += v[u];
+                    if (b0 + u * (256 / EP) < (int)blockIdx.x) p += v[u];
+                }
             }
         if (a) atomicAdd(&tot[e], a);
         if (p) atomicAdd(&pre[e], p);
