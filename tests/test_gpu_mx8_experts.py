@@ -105,7 +105,8 @@ CASES = [(1, 32, 1, 32, 1, "32x32/4", "32x32/4"), (5, 64, 3, 96, 9, "32x32/4", "
 # ... where the oracle looks at some rows
 LARGE = [(500, 128, 2, 4352, 8100, "256x256/8", "128x128/4"), (400, 384, 1, 8832, 4000, "256x256/8", "128x128/4"),
          (700, 1024, 3, 128, 8200, "128x128/4", "256x256/4"), (300, 4480, 2, 256, 2600, "128x128/4", "256x256/4"),
-         (900, 1152, 5, 4736, 9000, "256x256/8", "256x256/4")]
+         (900, 1152, 5, 4736, 9000, "256x256/8", "256x256/4"), (300, 768, 16, 384, 5998, "128x128/4", "192x128/4"),
+         (200, 1024, 8, 1408, 4000, "128x128/4", "192x128/4"), (300, 640, 10, 640, 6000, "128x128/4", "192x128/4")]
 
 
 @pytest.mark.parametrize("T,d,E,F,P,first,second", CASES)
