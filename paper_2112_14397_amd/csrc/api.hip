@@ -74,6 +74,12 @@ evomoe_status check_topk(const evomoe_topk* o, int E) {
         evomoe_status st_ = check_shape(shape);            \
         if (st_ != EVOMOE_OK) return st_;                  \
     } while (0)
+// ... and for the operators beside the DTS gate, whose kernels step over tokens with 32-bit counters
+#define CHECK_CTX_BLOCK()                                           \
+    do {                                                            \
+        CHECK_CTX_SHAPE();                                          \
+        if (shape->T > (1 << 30)) return EVOMOE_EUNSUPPORTED;       \
+    } while (0)
 
 evomoe_status from_hip(hipError_t e) { return e == hipSuccess ? EVOMOE_OK : EVOMOE_EHIP; }
 
@@ -425,7 +431,7 @@ evomoe_status evomoe_diversify(evomoe_ctx* ctx, const evomoe_shape* shape, const
 
 evomoe_status evomoe_gate_logits(evomoe_ctx* ctx, const evomoe_shape* shape, const void* x, const float* Wg,
                                  const float* bg, float* logits) {
-    CHECK_CTX_SHAPE();
+    CHECK_CTX_BLOCK();
     REQUIRE_PTR(x); REQUIRE_PTR(Wg); REQUIRE_PTR(logits); OPTIONAL_PTR(bg);
     ON_DEVICE();
     if (shape->dtype == EVOMOE_BF16) {
@@ -438,7 +444,7 @@ evomoe_status evomoe_gate_logits(evomoe_ctx* ctx, const evomoe_shape* shape, con
 evomoe_status evomoe_gate_logits_bwd(evomoe_ctx* ctx, const evomoe_shape* shape, const float* dlogits, const void* x,
                                      const float* Wg, const void* dx_in, float* dWg, float* dbg, void* dx,
                                      void* workspace, size_t workspace_bytes) {
-    CHECK_CTX_SHAPE();
+    CHECK_CTX_BLOCK();
     REQUIRE_PTR(dlogits); REQUIRE_PTR(x); REQUIRE_PTR(Wg); REQUIRE_PTR(dWg); REQUIRE_PTR(dx);
     OPTIONAL_PTR(dx_in); OPTIONAL_PTR(dbg);
     if (!workspace || !aligned16(workspace) || workspace_bytes < gate_bwd_workspace_bytes(*shape))
@@ -450,7 +456,7 @@ evomoe_status evomoe_gate_logits_bwd(evomoe_ctx* ctx, const evomoe_shape* shape,
 evomoe_status evomoe_topk_gate(evomoe_ctx* ctx, const evomoe_shape* shape, const evomoe_topk* topk, const float* logits,
                                const float* balance_bias, float* scores, float* gate_w, uint64_t* mask_bits,
                                int32_t* counts, int32_t* k_per_token, int32_t* block_hist) {
-    CHECK_CTX_SHAPE();
+    CHECK_CTX_BLOCK();
     if (evomoe_status st = check_topk(topk, shape->E); st != EVOMOE_OK) return st;
     REQUIRE_PTR(logits); REQUIRE_PTR(gate_w); REQUIRE_PTR(mask_bits); REQUIRE_PTR(counts);
     OPTIONAL_PTR(balance_bias); OPTIONAL_PTR(scores); OPTIONAL_PTR(k_per_token); OPTIONAL_PTR(block_hist);
@@ -463,7 +469,7 @@ evomoe_status evomoe_topk_gate_bwd(evomoe_ctx* ctx, const evomoe_shape* shape, c
                                    const float* dG_pairs, const int32_t* tok_off, const int32_t* tok_rows,
                                    const float* logits, const uint64_t* mask_bits, const float* dscore_coef,
                                    float loss_scale, float* dlogits) {
-    CHECK_CTX_SHAPE();
+    CHECK_CTX_BLOCK();
     if (evomoe_status st = check_topk(topk, shape->E); st != EVOMOE_OK) return st;
     REQUIRE_PTR(dG_pairs); REQUIRE_PTR(tok_off); REQUIRE_PTR(tok_rows); REQUIRE_PTR(logits); REQUIRE_PTR(mask_bits);
     REQUIRE_PTR(dlogits);
@@ -476,11 +482,14 @@ evomoe_status evomoe_topk_gate_bwd(evomoe_ctx* ctx, const evomoe_shape* shape, c
 evomoe_status evomoe_add_rmsnorm(evomoe_ctx* ctx, const evomoe_shape* shape, const void* x, const void* residual,
                                  const float* gamma, float eps, void* h, void* y, float* rstd, void* q,
                                  uint8_t* q_scale) {
-    CHECK_CTX_SHAPE();
+    CHECK_CTX_BLOCK();
     REQUIRE_PTR(x); REQUIRE_PTR(gamma);
     OPTIONAL_PTR(residual); OPTIONAL_PTR(h); OPTIONAL_PTR(y); OPTIONAL_PTR(rstd); OPTIONAL_PTR(q); OPTIONAL_PTR(q_scale);
-    if (!(eps > 0.f) || !(eps < INFINITY) || (!h && !y && !q) || (q != nullptr) != (q_scale != nullptr) || (h && h == y))
-        return EVOMOE_EINVAL;
+    if (!(eps > 0.f) || !(eps < INFINITY) || (!h && !y && !q) || (q != nullptr) != (q_scale != nullptr)) return EVOMOE_EINVAL;
+    const void* const outs[] = {h, y, q, q_scale, rstd};
+    for (int i = 0; i < 5; ++i)
+        for (int j = 0; j < i; ++j)
+            if (outs[i] && outs[i] == outs[j]) return EVOMOE_EINVAL;
     if (q && shape->d % 32) return EVOMOE_EUNSUPPORTED;
     ON_DEVICE();
     return from_hip(launch_add_rmsnorm(ctx->c, *shape, x, residual, gamma, eps, h, y, rstd, q, q_scale));
@@ -489,7 +498,7 @@ evomoe_status evomoe_add_rmsnorm(evomoe_ctx* ctx, const evomoe_shape* shape, con
 evomoe_status evomoe_add_rmsnorm_bwd(evomoe_ctx* ctx, const evomoe_shape* shape, const void* dy, const void* dh,
                                      const void* h, const float* gamma, const float* rstd, void* dx, float* dgamma,
                                      void* workspace, size_t workspace_bytes) {
-    CHECK_CTX_SHAPE();
+    CHECK_CTX_BLOCK();
     REQUIRE_PTR(dy); REQUIRE_PTR(h); REQUIRE_PTR(gamma); REQUIRE_PTR(rstd); REQUIRE_PTR(dx);
     OPTIONAL_PTR(dh); OPTIONAL_PTR(dgamma);
     if (dgamma && (!workspace || !aligned16(workspace) || workspace_bytes < rmsnorm_bwd_workspace_bytes(*shape)))

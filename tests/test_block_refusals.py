@@ -37,7 +37,7 @@ GOOD = {
     "evomoe_gate_logits_bwd": [A] * 8 + [BIG],
     "evomoe_topk_gate": [topk()] + [A] * 8,
     "evomoe_topk_gate_bwd": [topk()] + [A] * 6 + [1.0, A],
-    "evomoe_add_rmsnorm": [A, A, A, 1e-5, A, 2 * A, A, A, A],
+    "evomoe_add_rmsnorm": [A, A, A, 1e-5, A, 2 * A, 3 * A, 4 * A, 5 * A],
     "evomoe_add_rmsnorm_bwd": [A] * 8 + [BIG],
     "evomoe_expert_ffn_mx8": [A] * 12 + [BIG],
 }
@@ -77,7 +77,8 @@ def test_null_and_misaligned_arguments(name):
 @pytest.mark.parametrize("name", sorted(GOOD))
 @pytest.mark.parametrize("bad,status", [(dict(T=0), B.EVOMOE_EINVAL), (dict(d=-64), B.EVOMOE_EINVAL), (dict(E=0), B.EVOMOE_EINVAL),
                                         (dict(P=0), B.EVOMOE_EINVAL), (dict(E=65), B.EVOMOE_EUNSUPPORTED),
-                                        (dict(d=68), B.EVOMOE_EUNSUPPORTED), (dict(T=1 << 29), B.EVOMOE_EUNSUPPORTED)])
+                                        (dict(d=68), B.EVOMOE_EUNSUPPORTED), (dict(T=1 << 29), B.EVOMOE_EUNSUPPORTED),
+                                        (dict(T=(1 << 30) + 1, E=1), B.EVOMOE_EUNSUPPORTED)])
 def test_shapes(name, bad, status):
     assert call(name, shape(**bad), marshalled(GOOD[name])) == status
 
@@ -101,7 +102,10 @@ def test_norm_arguments():
     assert call("evomoe_add_rmsnorm", shape(), one(y=A, q=A)) == B.EVOMOE_EINVAL             # 8 bits without scales
     assert call("evomoe_add_rmsnorm", shape(), one(y=A, qs=A)) == B.EVOMOE_EINVAL
     assert call("evomoe_add_rmsnorm", shape(), one(h=A, y=A)) == B.EVOMOE_EINVAL             # one place for two outputs
-    assert call("evomoe_add_rmsnorm", shape(d=72), one(q=A, qs=A)) == B.EVOMOE_EUNSUPPORTED
+    assert call("evomoe_add_rmsnorm", shape(), one(y=A, q=A, qs=2 * A)) == B.EVOMOE_EINVAL
+    assert call("evomoe_add_rmsnorm", shape(), one(h=A, q=2 * A, qs=A)) == B.EVOMOE_EINVAL
+    assert call("evomoe_add_rmsnorm", shape(), one(y=A, rstd=A)) == B.EVOMOE_EINVAL
+    assert call("evomoe_add_rmsnorm", shape(d=72), one(q=A, qs=2 * A)) == B.EVOMOE_EUNSUPPORTED
 
 
 def test_quantize_arguments():
