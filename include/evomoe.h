@@ -387,7 +387,7 @@ evomoe_status evomoe_quantize_mx8(evomoe_ctx* ctx, int64_t rows, int64_t cols, i
  *        W2_scale [E,d,F/32], b2 [E,d] f32 (NULL = 0).
  *   out: O [P_cap,d] bf16, rows below P only.
  *   workspace: at least evomoe_workspace_bytes_mx8(shape) bytes (evomoe_workspace_bytes is more than that).
- * Limits: dtype bf16; d and F multiples of 32; T*max(d,F) and d*F below 2^32. */
+ * Limits: dtype bf16; d and F multiples of 32; T*max(d,F) and d*F below 2^32; d and F up to 2^24. */
 size_t evomoe_workspace_bytes_mx8(const evomoe_shape* shape);
 evomoe_status evomoe_expert_ffn_mx8(evomoe_ctx* ctx, const evomoe_shape* shape,
                                     const void* x_q, const uint8_t* x_scale,

@@ -35,12 +35,13 @@ evomoe_status check_ffn_shape(const evomoe_shape* s) {
     return EVOMOE_OK;
 }
 
-// Limits of the 8-bit expert FFN: bf16 layers, whole groups of 32, 32-bit byte offsets inside a tile's operands.
+// Limits of the 8-bit expert FFN: bf16 layers, whole groups of 32, 32-bit byte offsets inside a tile's operands, and 30-bit ones inside
+// 32 rows of its output.
 evomoe_status check_mx8_shape(const evomoe_shape* s) {
     if (evomoe_status st = check_shape(s); st != EVOMOE_OK) return st;
     const int64_t lim = (int64_t)1 << 32, wide = s->d > s->F ? s->d : s->F;
     if (s->dtype != EVOMOE_BF16 || s->d % 32 || s->F % 32) return EVOMOE_EUNSUPPORTED;
-    if ((int64_t)s->T * wide >= lim || (int64_t)s->d * s->F >= lim) return EVOMOE_EUNSUPPORTED;
+    if ((int64_t)s->T * wide >= lim || (int64_t)s->d * s->F >= lim || wide > (1 << 24)) return EVOMOE_EUNSUPPORTED;
     return EVOMOE_OK;
 }
 

@@ -120,7 +120,8 @@ def test_quantize_arguments():
 
 def test_limits_of_the_8_bit_experts():
     args = GOOD["evomoe_expert_ffn_mx8"]
-    for bad in (dict(dtype=F32), dict(d=72), dict(F=104), dict(d=65536, F=65536), dict(T=1 << 22, d=1024)):
+    for bad in (dict(dtype=F32), dict(d=72), dict(F=104), dict(d=65536, F=65536), dict(T=1 << 22, d=1024),
+                dict(T=2, d=(1 << 24) + 128, F=128), dict(T=2, d=128, F=(1 << 24) + 128)):
         assert call("evomoe_expert_ffn_mx8", shape(**bad), args) == B.EVOMOE_EUNSUPPORTED
         assert B.evomoe_workspace_bytes_mx8(shape(**bad)) == 0
     for P in (1, 100, 59000):
