@@ -482,9 +482,9 @@ hipError_t launch_topk_gate(const Ctx& c, const evomoe_shape& s, const evomoe_to
     return with_lanes(s.E, [&](auto lanes) {
         constexpr int LPT = decltype(lanes)::value;
         // Blocks of 256 tokens, dispatch's unit, write their rows of block_hist outright; where they would leave CUs idle, smaller ones add
-        // to cleared rows (32768 tokens, 64 experts, k 8, in groups: 39 us in 256 blocks, 43 in 128).
+        // to cleared rows, or without them to the counts (32768 tokens, 64 experts, k 8, in groups: 39 us in 256 blocks, 43 in 128).
         TopkArgs b = a;
-        while (block_hist && s.T > b.span && b.span > kTopkThreads<LPT> / LPT && (s.T - 1) / b.span + 1 <= c.num_cu / 2) b.span /= 2;
+        while (s.T > b.span && b.span > kTopkThreads<LPT> / LPT && (s.T - 1) / b.span + 1 <= c.num_cu / 2) b.span /= 2;
         const int blocks = (s.T - 1) / b.span + 1;
         if (b.span < kDispatchTokens || (blocks > 1 && !block_hist)) {
             hipError_t err = launch_clear_counts(c, s, counts, block_hist);

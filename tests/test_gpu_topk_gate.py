@@ -179,3 +179,15 @@ def test_optional_outputs_and_rows_that_do_not_fit(ctx):
     with pytest.raises(B.EvoMoEError) as e:                # the capacity flag is reported, and cleared
         B.evomoe_num_pairs(ctx, torch.zeros(1, dtype=torch.int64, device="cuda"))
     assert e.value.status == B.EVOMOE_ECAPACITY
+
+
+@pytest.mark.parametrize("T,E", [(257, 64), (2000, 40), (40000, 33)])
+def test_counts_without_the_histogram(ctx, T, E):
+    rng = np.random.default_rng(T)
+    z, o = rng.standard_normal((T, E)).astype(np.float32), blk.TopK(5, "sigmoid")
+    gw, mask, counts = torch.empty(T, E, device="cuda"), torch.empty(T, dtype=torch.int64, device="cuda"), torch.full((E,), 7, dtype=torch.int32, device="cuda")
+    for _ in range(2):
+        B.evomoe_topk_gate(ctx, B.make_shape(T, 64, E, 64, "f32", "relu", 1), gpu_topk(o), torch.from_numpy(z).cuda(), None, None, gw, mask, counts)
+        want = blk.topk_select(z, None, o)
+        assert np.array_equal(mask.cpu().numpy().view(np.uint64), bits_of(want))
+        assert np.array_equal(counts.cpu().numpy(), want.sum(0))
