@@ -99,17 +99,16 @@ evomoe_status ensure_scratch(Ctx& c, size_t elems) {
     return EVOMOE_OK;
 }
 
-// Scratch of the bf16 gate (split copy of W_g); grows with a device allocation when a larger d*E shows up.
+// Scratch of the bf16 gate (split copy of W_g); grows with a device allocation when a larger d shows up, to twice the size at least.  The
+// smaller one is kept until the context ends, as a captured graph may go on using it.
 evomoe_status ensure_wg_planes(Ctx& c, size_t bytes) {
     if (bytes <= c.wg_planes_bytes) return EVOMOE_OK;
-    if (c.wg_planes) {
-        if (hipStreamSynchronize(c.stream) != hipSuccess) return EVOMOE_EHIP;
-        if (hipFree(c.wg_planes) != hipSuccess) return EVOMOE_EHIP;
-        c.wg_planes = nullptr;
-        c.wg_planes_bytes = 0;
-    }
-    const size_t want = bytes < (1u << 20) ? (1u << 20) : bytes;
-    if (hipMalloc(&c.wg_planes, want) != hipSuccess) return EVOMOE_EHIP;
+    size_t want = c.wg_planes ? 2 * c.wg_planes_bytes : (size_t)1 << 20;
+    if (want < bytes) want = bytes;
+    uint16_t* planes = nullptr;
+    if (c.wg_olds == 32 || hipMalloc(&planes, want) != hipSuccess) return EVOMOE_EHIP;
+    if (c.wg_planes) c.wg_old[c.wg_olds++] = c.wg_planes;
+    c.wg_planes = planes;
     c.wg_planes_bytes = want;
     return EVOMOE_OK;
 }
@@ -129,6 +128,7 @@ evomoe_status evomoe_create(evomoe_ctx** ctx_out, void* hip_stream) {
     c.block_counts_elems = 0;
     c.wg_planes = nullptr;
     c.wg_planes_bytes = 0;
+    c.wg_olds = 0;
     c.status_dev = nullptr;
     c.prof = nullptr;
     c.pair_hint = 0;
@@ -159,6 +159,7 @@ evomoe_status evomoe_destroy(evomoe_ctx* ctx) {
     (void)hipStreamSynchronize(ctx->c.stream);
     if (ctx->c.block_counts) (void)hipFree(ctx->c.block_counts);
     if (ctx->c.wg_planes) (void)hipFree(ctx->c.wg_planes);
+    for (int i = 0; i < ctx->c.wg_olds; ++i) (void)hipFree(ctx->c.wg_old[i]);
     if (ctx->c.status_dev) (void)hipFree(ctx->c.status_dev);
     if (ctx->c.prof) {
         for (int i = 0; i < ctx->c.prof->cap; ++i) {

@@ -134,6 +134,8 @@ struct Ctx {
     size_t block_counts_elems;
     uint16_t* wg_planes;      // bf16 gate: W_g split into three bf16 terms, in MFMA fragment order
     size_t wg_planes_bytes;
+    uint16_t* wg_old[32];     // smaller ones before it: graphs captured with them still use them
+    int wg_olds;
     Prof* prof;
 };
 

@@ -71,3 +71,34 @@ def test_the_dts_gate_s_softmax_follows_from_the_logits(dtype):
     # the same products and sums; / tau is exact, the softmax rounds as in the top-k gate's test (spread below 16)
     assert (gp.double() - torch.softmax(z.double() / 0.5, 1)).abs().max().item() <= U * 32
     ctx.close()
+
+
+def test_a_captured_pass_outlives_a_larger_one():
+    """The split copy of W_g grows with d; a graph that was captured before goes on with the smaller one."""
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        g = torch.Generator(device="cuda").manual_seed(3)
+        ctx, new = B.Context(), lambda *s: torch.randn(*s, generator=g, device="cuda")
+        T, d, E = 5000, 64, 16
+        shape, x, W, z = B.make_shape(T, d, E, d, "bf16", "gelu", 1), new(T, d).bfloat16(), new(d, E), new(T, E)
+        B.evomoe_gate_logits(ctx, shape, x, W, None, z)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            B.evomoe_gate_logits(ctx, shape, x, W, None, z)
+        wide = 8192
+        x2, W2, z2 = new(T, wide).bfloat16(), new(wide, E), new(T, E)
+        B.evomoe_gate_logits(ctx, B.make_shape(T, wide, E, wide, "bf16", "gelu", 1), x2, W2, None, z2)
+        mine = B.Context()
+        for i in range(3):
+            x.copy_(new(T, d))
+            W.copy_(new(d, E))
+            graph.replay()
+            torch.randn(2048, 2048, device="cuda").sum()
+            want = torch.empty_like(z)
+            B.evomoe_gate_logits(mine, shape, x, W, None, want)
+            torch.cuda.synchronize()
+            assert torch.equal(z, want)
+        torch.cuda.synchronize()
+        ctx.close()
+        mine.close()
