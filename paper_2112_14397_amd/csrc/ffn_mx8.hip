@@ -506,11 +506,14 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
 // (128x64 each, two to a SIMD): they fill each other's stalls in an epilogue that gelu and conversion make as long as the main loop.
 // MID: 128x128, two blocks per unit, one's epilogue under the other's products.  DEEP: 128x128 with four slabs on their way, for
 // long contractions with few tiles.  TALL: 192x128, three slabs, where DEEP's tiles begin another round on the CUs and TALL's do not.
-// SML: 64x128.  us, E = 16, d = 768, F = 3072 (but for the last row) / E = 64, d = 1024, F = 4096:
+// SML: 64x128.  LOW: the same with four slabs, as long as its tiles are one round; SLIM: 64x64, for up to 16 rows an expert, where half as
+// many places would be in use.  us, E = 16, d = 768, F = 3072 (but for the last row) / E = 64, d = 1024, F = 4096:
 //   first product, pairs   48   512  2048  5998 16384 65536 /    96 65536    second product   48   512  2048  5998 16384 65536 / 65536
 //     SML                 13.0  14.4  20.6  40.6  96.2   359 /  48.5   575                   20.4  21.0  22.9  44.6  79.1   315 /   542
 //     MID                 14.8  16.2  21.9  37.0  79.9   281 /  52.6   467                   20.8  21.7  24.4  47.6  60.9   230 /   391
 //     DEEP                20.0  20.3  27.7  44.2   104   381 /  66.9   561                   16.7  17.2  20.5  36.7  67.1   244 /   416
+//     SLIM                  -     -     -     -     -     -     /    -     -                     12.2  17.4  18.3    -     -     -  /    -
+//     LOW                   -     -     -     -     -     -     /    -     -                     15.1  15.7  17.6    -     -     -  /    -
 //     TALL                  -     -     -     -     -     -     /    -     -                     20.5  20.5  23.1  27.6  68.2   227 /   392
 //     BIG                   -   23.4  25.1  44.0  84.1   276 /    -    445                     -   36.2  38.1  42.8  49.6   207 /   325
 //     BIG8                  -   21.8  23.9  40.8  77.2   256 /    -    420                     -   35.3  37.8  42.2  50.5   218 /   342
@@ -523,8 +526,10 @@ struct Mid { static constexpr int BX = 128, BW = 128, WX = 2, WW = 2, NST = 2, W
 struct Deep { static constexpr int BX = 128, BW = 128, WX = 2, WW = 2, NST = 4, WPE = 1, BLOCKS = 1; };
 struct Sml { static constexpr int BX = 64, BW = 128, WX = 2, WW = 2, NST = 2, WPE = 2, BLOCKS = 2; };
 struct Tall { static constexpr int BX = 192, BW = 128, WX = 2, WW = 2, NST = 3, WPE = 1, BLOCKS = 1; };
+struct Slim { static constexpr int BX = 64, BW = 64, WX = 2, WW = 2, NST = 4, WPE = 2, BLOCKS = 2; };
+struct Low { static constexpr int BX = 64, BW = 128, WX = 2, WW = 2, NST = 4, WPE = 1, BLOCKS = 1; };
 
-enum class Pick { FewRows, Sml, Mid, Deep, Tall, Big, Big8 };
+enum class Pick { FewRows, Sml, Mid, Slim, Low, Deep, Tall, Big, Big8 };
 Pick pick(const Ctx& c, const evomoe_shape& s, bool first) {
     const int64_t pairs = c.pair_hint > 0 && c.pair_hint < s.P_cap ? c.pair_hint : s.P_cap, weights = (int64_t)s.d * s.F;
     if (s.d % 128 || s.F % 128 || (pairs <= s.E && pairs * weights <= 40000000)) return Pick::FewRows;
@@ -532,8 +537,10 @@ Pick pick(const Ctx& c, const evomoe_shape& s, bool first) {
     const int n = first ? s.F : s.d;
     const int64_t tiles = ((pairs + 255) / 256 + s.E / 2) * ((n + 255) / 256);
     if (pairs >= 512 * s.E && tiles >= (first ? 2 * c.num_cu : c.num_cu / 2)) return first ? Pick::Big8 : Pick::Big;
-    if (!first) {     // a DEEP tile takes two thirds of a TALL one's time
+    if (!first) {     // (a DEEP tile takes two thirds of a TALL one's time)
+        if (pairs <= 16 * s.E) return Pick::Slim;
         auto rounds = [&](int64_t rows) { return (((pairs + rows - 1) / rows + s.E / 2) * ((n + 127) / 128) + c.num_cu - 1) / c.num_cu; };
+        if (rounds(Low::BX) == 1) return Pick::Low;
         return 3 * rounds(Tall::BX) < 2 * rounds(Deep::BX) ? Pick::Tall : Pick::Deep;
     }
     return pairs >= 256 * s.E ? Pick::Mid : Pick::Sml;
@@ -579,6 +586,8 @@ hipError_t launch_second(const Ctx& c, const evomoe_shape& s, const Mx8Args& a) 
     switch (pick(c, s, false)) {
         case Pick::FewRows: return launch_few_rows<TO_OUTPUT>(c, s, a);
         case Pick::Deep: return launch_tiles<TO_OUTPUT, Deep>(c, s, a);
+        case Pick::Slim: return launch_tiles<TO_OUTPUT, Slim>(c, s, a);
+        case Pick::Low: return launch_tiles<TO_OUTPUT, Low>(c, s, a);
         case Pick::Tall: return launch_tiles<TO_OUTPUT, Tall>(c, s, a);
         default: return launch_tiles<TO_OUTPUT, Big>(c, s, a);
     }
@@ -594,6 +603,8 @@ FfnTile mx8_ffn_tile(const Ctx& c, const evomoe_shape& s, int kernel) {
         case Pick::Sml: return {Sml::BX, Sml::BW, 4};
         case Pick::Mid: return {Mid::BX, Mid::BW, 4};
         case Pick::Deep: return {Deep::BX, Deep::BW, 4};
+        case Pick::Slim: return {Slim::BX, Slim::BW, 4};
+        case Pick::Low: return {Low::BX, Low::BW, 4};
         case Pick::Tall: return {Tall::BX, Tall::BW, 4};
         case Pick::Big: return {Big::BX, Big::BW, 4};
         case Pick::Big8: return {Big8::BX, Big8::BW, 8};

@@ -23,4 +23,4 @@ def test_cases_reach_the_tiles_they_name_and_all_there_are():
         assert got == tuple(named), (T, d, E, F, P)
         for s, t in zip(seen, got):
             s.add(t)
-    assert seen == [{"32x32/4", "64x128/4", "128x128/4", "256x256/8"}, {"32x32/4", "128x128/4", "192x128/4", "256x256/4"}]
+    assert seen == [{"32x32/4", "64x128/4", "128x128/4", "256x256/8"}, {"32x32/4", "64x64/4", "64x128/4", "128x128/4", "192x128/4", "256x256/4"}]
