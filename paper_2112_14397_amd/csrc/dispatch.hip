@@ -81,20 +81,26 @@ __global__ __launch_bounds__(256) void dispatch_scatter_kernel(
     if (tid < 64) { pre[tid] = 0; tot[tid] = 0; }
     __syncthreads();
     {
+        constexpr int ROWS = 256 / EP;
         const int e = tid % EP, rl = tid / EP;
         int p = 0, a = 0;
         if (e < E)
-            for (int b0 = rl; b0 < nblk; b0 += 8 * (256 / EP)) {       // (eight rows on their way together)
-                int v[8];
+            for (int b0 = rl; b0 < nblk; b0 += 8 * ROWS) {
+                if (b0 - rl + 8 * ROWS <= nblk) {            // eight rows on their way together
+                    int v[8];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    const int b = b0 + u * (256 / EP);
-                    v[u] = b < nblk ? block_counts[(size_t)b * E + e] : 0;
-                }
+                    for (int u = 0; u < 8; ++u) v[u] = block_counts[(size_t)(b0 + u * ROWS) * E + e];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    a += v[u];
-                    if (b0 + u * (256 / EP) < (int)blockIdx.x) p += v[u];
+                    for (int u = 0; u < 8; ++u) {
+                        a += v[u];
+                        if (b0 + u * ROWS < (int)blockIdx.x) p += v[u];
+                    }
+                } else {
+                    for (int b = b0; b < nblk; b += ROWS) {
+                        const int v = block_counts[(size_t)b * E + e];
+                        a += v;
+                        if (b < (int)blockIdx.x) p += v;
+                    }
                 }
             }
         if (a) atomicAdd(&tot[e], a);
