@@ -460,47 +460,56 @@ hipError_t launch_dts_gate(const Ctx& c, const evomoe_shape& s, const void* x, c
                                  counts, k_per_token, block_hist);
 }
 
-// Logits alone of a bf16 layer's few tokens: one launch, in which 16 waves share the k-blocks of 16 tokens and split W_g themselves, as
+// Logits alone of few tokens: one launch, in which 16 waves share the k-slabs of 16 tokens; a bf16 layer's split W_g themselves, as
 // reading it 16 at a time costs less than a second launch.
-template <int NE>
-__global__ __launch_bounds__(1024) void logits_few_kernel(const bf16_t* __restrict__ x, const float* __restrict__ Wg,
+template <typename TX, int NE>
+__global__ __launch_bounds__(1024) void logits_few_kernel(const TX* __restrict__ x, const float* __restrict__ Wg,
                                                           const float* __restrict__ bg, int T, int d, int E, float* __restrict__ logits)
 {
-    constexpr int LDZ = 16 * NE, XU = 2;                     // k-blocks of a wave whose loads are on their way together
+    constexpr bool F32 = std::is_same<TX, float>::value;
+    constexpr int KV = Elem<TX>::kVec, KB = 4 * KV;          // k's of a lane's load and of a slab
+    constexpr int LDZ = 16 * NE, XU = F32 ? (NE == 4 ? 2 : 4) : (NE == 4 ? 1 : 2);   // slabs of a wave whose loads are on their way together
     __shared__ float part[16][16 * LDZ];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i16 = lane & 15, q = lane >> 4;
     const int t0 = blockIdx.x * 16, t = t0 + i16;
     f32x4 acc[NE];
 #pragma unroll
     for (int n = 0; n < NE; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int kb = wave; kb * 32 < d; kb += 16 * XU) {
-        bf16x8 a[XU];
-        float w[XU][NE][8];
+    for (int kb = wave; kb * KB < d; kb += 16 * XU) {
+        u32x4 a[XU];
+        float w[XU][NE][KV];
 #pragma unroll
         for (int u = 0; u < XU; ++u) {
-            const int k0 = (kb + 16 * u) * 32 + q * 8;       // (d is a multiple of 8)
-            a[u] = k0 < d && t < T ? *reinterpret_cast<const bf16x8*>(x + (size_t)t * d + k0) : bf16x8{};
+            const int k0 = (kb + 16 * u) * KB + q * KV;      // (d is a multiple of KV)
+            a[u] = k0 < d && t < T ? *reinterpret_cast<const u32x4*>(x + (size_t)t * d + k0) : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
             for (int n = 0; n < NE; ++n)
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
+                for (int j = 0; j < KV; ++j)
                     w[u][n][j] = k0 < d && n * 16 + i16 < E ? Wg[(size_t)(k0 + j) * E + n * 16 + i16] : 0.f;
         }
 #pragma unroll
         for (int u = 0; u < XU; ++u)
 #pragma unroll
             for (int n = 0; n < NE; ++n) {
-                bf16x8 hi, mid, lo;
+                if constexpr (F32) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    hi[j] = (bf16_t)w[u][n][j];
-                    const float r1 = w[u][n][j] - (float)hi[j];
-                    mid[j] = (bf16_t)r1;
-                    lo[j] = (bf16_t)(r1 - (float)mid[j]);
+                    for (int j = 0; j < KV; ++j)
+                        acc[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[u][j]), w[u][n][j], acc[n], 0, 0, 0);
+                } else {
+                    const bf16x8 xv = __builtin_bit_cast(bf16x8, a[u]);
+                    bf16x8 hi, mid, lo;
+#pragma unroll
+                    for (int j = 0; j < KV; ++j) {
+                        hi[j] = (bf16_t)w[u][n][j];
+                        const float r1 = w[u][n][j] - (float)hi[j];
+                        mid[j] = (bf16_t)r1;
+                        lo[j] = (bf16_t)(r1 - (float)mid[j]);
+                    }
+                    acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, lo, acc[n], 0, 0, 0);
+                    acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, mid, acc[n], 0, 0, 0);
+                    acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, hi, acc[n], 0, 0, 0);
                 }
-                acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[u], lo, acc[n], 0, 0, 0);
-                acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[u], mid, acc[n], 0, 0, 0);
-                acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[u], hi, acc[n], 0, 0, 0);
             }
     }
 #pragma unroll
@@ -517,16 +526,18 @@ __global__ __launch_bounds__(1024) void logits_few_kernel(const bf16_t* __restri
         logits[(size_t)t0 * E + i] = sum + (bg ? bg[e] : 0.f);
     }
 }
-// Whose blocks, one to 16 tokens, take no more than one trip over the CUs and for many experts less, as every block splits all of W_g
-// (us a call, one launch / two: T = 48, d = 768, E = 16 4.4 / 7.4, T = 4096 4.5 / 7.6; T = 256, d = 1024, E = 64 9.9 / 10.6, T = 1024
-// 10.6 / 10.5, T = 4096 14.1 / 11.9; T = 16384, d = 768, E = 32 19.9 / 13.5).
+// As long as its blocks, one to 16 tokens, are one round on the CUs; in float32 for five rounds where d fills the sixteen waves, as the other
+// kernel is slower there (us a call, this one / the other: bf16 T = 48, d = 768, E = 16 4.4 / 7.4, T = 4096 4.5 / 7.6, T = 4096, d = 1024,
+// E = 64 9.0 / 11.9, T = 8192, d = 512, E = 64 10.8 / 10.6, T = 16384, d = 768, E = 32 19.9 / 13.5; float32 T = 48, d = 768, E = 16 4.4 / 8.7,
+// T = 4096, d = 512, E = 64 7.3 / 17.4, T = 12000, d = 768, E = 48 23.2 / 34.4, T = 20000, d = 256, E = 48 29.7 / 19.3, T = 30000,
+// d = 1024, E = 64 90 / 85).
 static bool few_logits(const Ctx& c, const evomoe_shape& s) {
-    return s.dtype == EVOMOE_BF16 && (int64_t)s.T * ((s.E + 15) / 16) <= 16 * c.num_cu;
+    return s.T <= (s.dtype == EVOMOE_F32 && s.d >= 512 ? 80 : 16) * c.num_cu;
 }
-template <int NE>
+template <typename TX, int NE>
 static hipError_t logits_few_launch(const Ctx& c, const evomoe_shape& s, const void* x, const float* Wg, const float* bg, float* logits) {
     ProfScope ps(c, EVOMOE_K_GATE_LOGITS);
-    hipLaunchKernelGGL(logits_few_kernel<NE>, dim3((s.T + 15) / 16), dim3(1024), 0, c.stream, (const bf16_t*)x, Wg, bg, s.T, s.d, s.E,
+    hipLaunchKernelGGL((logits_few_kernel<TX, NE>), dim3((s.T + 15) / 16), dim3(1024), 0, c.stream, (const TX*)x, Wg, bg, s.T, s.d, s.E,
                        logits);
     return hipGetLastError();
 }
@@ -556,7 +567,7 @@ static hipError_t logits_launch(const Ctx& c, const evomoe_shape& s, const void*
     const int rt = pick_rt(c, s);
     auto with = [&](auto ne) {
         constexpr int NE = decltype(ne)::value;
-        if (few_logits(c, s)) return logits_few_launch<NE>(c, s, x, Wg, bg, logits);
+        if (few_logits(c, s)) return logits_few_launch<TX, NE>(c, s, x, Wg, bg, logits);
         return rt == 4 ? logits_launch_t<TX, NE, 4>(c, s, x, Wg, bg, logits)
              : rt == 2 ? logits_launch_t<TX, NE, 2>(c, s, x, Wg, bg, logits)
                        : logits_launch_t<TX, NE, 1>(c, s, x, Wg, bg, logits);
@@ -928,6 +939,108 @@ __global__ __launch_bounds__(256, 2) void gate_bwd_mfma_kernel(
     if (slice == 0 && tid < E) dbg_part[(size_t)blk * (d + 1) * E + tid] = sb;
 }
 
+// ---- float32 logits: the same two contractions on v_mfma_f32_32x32x2_f32, whose products and sums are float32's ----
+//   lane (h = lane / 32, i = lane % 32) brings row i, k = h of the one operand and k = h, column i of the other, and receives rows
+//   8 (r / 4) + 4 h + r % 4 of column i: x, dx_in and dx are read and written straight from and to memory, 32 neighbours of a token's row at
+//   a time; only dz goes through the LDS, as tokens are the rows of the one product and the k's of the other.
+// Block = 4 waves = one run of tokens x 128 columns (32 per wave), in chunks of 32 tokens, the next chunk's loads under the present one's
+// products.  NE = tiles of 32 experts.  us with two events, this kernel / gate_bwd_kernel: T = 48, d = 768, E = 16 8.7 / 20.2, T = 2048,
+// d = 512, E = 32 10.9 / 36.0, T = 8192, d = 512, E = 64 28 / 85, T = 20000, d = 1024, E = 16 55 / 85 (246 MB: memory).
+struct LbPlan { int slices, tokens_per_block, nblk; };
+LbPlan logits_bwd_f32_plan(const evomoe_shape& s) {
+    LbPlan p;
+    p.slices = (s.d + 127) / 128;
+    int n = 768 / p.slices;                          // about three waves per SIMD
+    const int cap = s.T / s.E > 32 ? s.T / s.E : 32; // bounds the partial dWg tables by the size of x
+    if (n > cap) n = cap;
+    if (n > 256) n = 256;
+    if (n < 1) n = 1;
+    p.tokens_per_block = ((s.T + n - 1) / n + 31) / 32 * 32;
+    p.nblk = (s.T + p.tokens_per_block - 1) / p.tokens_per_block;
+    return p;
+}
+
+template <int NE>
+__global__ __launch_bounds__(256) void logits_bwd_f32_kernel(
+    const float* __restrict__ dz, const float* __restrict__ x, const float* __restrict__ Wg, int T, int d, int E, int tokens_per_block,
+    const float* dx_in, float* dx, float* __restrict__ dWg_part, float* __restrict__ dbg_part)
+{
+    constexpr int LD = 32 * NE + 1, DZN = 32 * 32 * NE / 256;
+    __shared__ float sdz[32 * LD];                   // [token][expert], zero beyond
+    const int tid = threadIdx.x, lane = tid & 63, i32 = lane & 31, h = lane >> 5;
+    const int col = blockIdx.y * 128 + (tid >> 6) * 32 + i32;
+    const bool col_ok = col < d;
+    const int s_begin = blockIdx.x * tokens_per_block, s_end = min(T, s_begin + tokens_per_block);
+
+    float w[16 * NE];                                // W_g[col][2 k + h]
+#pragma unroll
+    for (int k = 0; k < 16 * NE; ++k) w[k] = col_ok && 2 * k + h < E ? Wg[(size_t)col * E + 2 * k + h] : 0.f;
+    f32x16 acc_w[NE];
+#pragma unroll
+    for (int n = 0; n < NE; ++n) acc_w[n] = f32x16{};
+    float sb = 0.f;                                  // bias gradient partial (thread = expert)
+
+    float xv[16], in[16], zv[DZN];
+    auto load = [&](int s0) {
+#pragma unroll
+        for (int u = 0; u < DZN; ++u) {
+            const int i = tid + 256 * u, t = s0 + i / (32 * NE), e = i % (32 * NE);
+            zv[u] = t < s_end && e < E ? dz[(size_t)t * E + e] : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const int t = s0 + 2 * k + h;
+            xv[k] = col_ok && t < s_end ? x[(size_t)t * d + col] : 0.f;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int t = s0 + 8 * (r >> 2) + 4 * h + (r & 3);
+            in[r] = dx_in && col_ok && t < s_end ? dx_in[(size_t)t * d + col] : 0.f;
+        }
+    };
+    load(s_begin);
+    for (int s0 = s_begin; s0 < s_end; s0 += 32) {
+        __syncthreads();                             // the previous chunk's readers are done
+#pragma unroll
+        for (int u = 0; u < DZN; ++u) {
+            const int i = tid + 256 * u;
+            sdz[i / (32 * NE) * LD + i % (32 * NE)] = zv[u];
+        }
+        f32x16 acc_x;
+        float xc[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) { acc_x[r] = in[r]; xc[r] = xv[r]; }
+        __syncthreads();
+        if (s0 + 32 < s_end) load(s0 + 32);
+        if (blockIdx.y == 0 && tid < E)
+            for (int t = 0; t < 32; ++t) sb += sdz[t * LD + tid];
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+#pragma unroll
+            for (int n = 0; n < NE; ++n)
+                acc_w[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(xc[k], sdz[(2 * k + h) * LD + n * 32 + i32], acc_w[n], 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < 16 * NE; ++k)            // (experts beyond E: 0 by 0)
+            acc_x = __builtin_amdgcn_mfma_f32_32x32x2f32(sdz[i32 * LD + 2 * k + h], w[k], acc_x, 0, 0, 0);
+        asm volatile("" : "+v"(acc_x));              // (not to be moved under the stores' branch)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int t = s0 + 8 * (r >> 2) + 4 * h + (r & 3);
+            if (col_ok && t < s_end) dx[(size_t)t * d + col] = acc_x[r];
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NE; ++n) {
+        asm volatile("" : "+v"(acc_w[n]));
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int k = blockIdx.y * 128 + (tid >> 6) * 32 + 8 * (r >> 2) + 4 * h + (r & 3), e = n * 32 + i32;
+            if (k < d && e < E) dWg_part[((size_t)blockIdx.x * (d + 1) + k) * E + e] = acc_w[n][r];
+        }
+    }
+    if (blockIdx.y == 0 && tid < E) dbg_part[(size_t)blockIdx.x * (d + 1) * E + tid] = sb;
+}
+
 bool gate_bwd_use_mfma(const evomoe_shape& s) { return s.dtype == EVOMOE_BF16; }   // (d is a multiple of 8 there)
 
 }  // namespace
@@ -976,6 +1089,7 @@ size_t gate_bwd_workspace_bytes(const evomoe_shape& s) {
     const int tc = gate_bwd_chunk_tokens(s);
     size_t nchunk = (s.T + tc - 1) / tc;
     if (gate_bwd_use_mfma(s)) nchunk = gate_bwd_mfma_plan(s).nblk;
+    else if ((size_t)logits_bwd_f32_plan(s).nblk > nchunk) nchunk = logits_bwd_f32_plan(s).nblk;
     return ((size_t)s.T * s.E + nchunk * ((size_t)s.d * s.E + s.E)) * sizeof(float);
 }
 
@@ -1006,12 +1120,13 @@ static hipError_t gate_bwd_t(const Ctx& c, const evomoe_shape& s, const float* d
 }
 
 // part: chunk c's partial sums, [dWg partial: d x E][dbg partial: E], contiguous
-hipError_t launch_gate_logits_bwd(const Ctx& c, const evomoe_shape& s, const float* dz, const void* x, const float* Wg,
-                                  const void* dx_in, float* dWg, float* dbg, void* dx, float* part) {
+static hipError_t gate_bwd_contract(const Ctx& c, const evomoe_shape& s, const float* dz, const void* x, const float* Wg,
+                                    const void* dx_in, float* dWg, float* dbg, void* dx, float* part, bool logits) {
     const int tc = gate_bwd_chunk_tokens(s);
     const bool mfma = gate_bwd_use_mfma(s);
     const GbPlan plan = gate_bwd_mfma_plan(s);
-    const int nchunk = mfma ? plan.nblk : (s.T + tc - 1) / tc;
+    const LbPlan lplan = logits_bwd_f32_plan(s);
+    const int nchunk = mfma ? plan.nblk : logits ? lplan.nblk : (s.T + tc - 1) / tc;
     float* dbg_part = part + (size_t)s.d * s.E;
     hipError_t err;
     {
@@ -1027,6 +1142,11 @@ hipError_t launch_gate_logits_bwd(const Ctx& c, const evomoe_shape& s, const flo
             else EVOMOE_GBM(4, 2);
 #undef EVOMOE_GBM
             err = hipGetLastError();
+        } else if (logits) {
+            auto kern = s.E <= 32 ? logits_bwd_f32_kernel<1> : logits_bwd_f32_kernel<2>;
+            hipLaunchKernelGGL(kern, dim3(lplan.nblk, lplan.slices), dim3(256), 0, c.stream, dz, (const float*)x, Wg, s.T, s.d, s.E,
+                               lplan.tokens_per_block, (const float*)dx_in, (float*)dx, part, dbg_part);
+            err = hipGetLastError();
         } else {
             err = gate_bwd_t<float>(c, s, dz, x, Wg, dx_in, dx, part, dbg_part, tc, nchunk);
         }
@@ -1037,6 +1157,11 @@ hipError_t launch_gate_logits_bwd(const Ctx& c, const evomoe_shape& s, const flo
     hipLaunchKernelGGL(sum_chunks_kernel, dim3((n0 + n1 + 63) / 64), dim3(256), 0, c.stream, part, nchunk, n0,
                        n1, dWg, dbg);
     return hipGetLastError();
+}
+
+hipError_t launch_gate_logits_bwd(const Ctx& c, const evomoe_shape& s, const float* dz, const void* x, const float* Wg,
+                                  const void* dx_in, float* dWg, float* dbg, void* dx, float* part) {
+    return gate_bwd_contract(c, s, dz, x, Wg, dx_in, dWg, dbg, dx, part, true);
 }
 
 hipError_t launch_dts_gate_bwd(const Ctx& c, const evomoe_shape& s, const float* dG_pairs,
@@ -1060,7 +1185,7 @@ hipError_t launch_dts_gate_bwd(const Ctx& c, const evomoe_shape& s, const float*
     }
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    return launch_gate_logits_bwd(c, s, dz, x, Wg, dx, dWg, dbg, dx, dz + (size_t)s.T * s.E);
+    return gate_bwd_contract(c, s, dz, x, Wg, dx, dWg, dbg, dx, dz + (size_t)s.T * s.E, false);
 }
 
 // ---------------------------------------------------------------------------------------------

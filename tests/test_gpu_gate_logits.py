@@ -12,7 +12,8 @@ pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
 CASES = [("bf16", 1, 64, 1), ("bf16", 5, 8, 64), ("bf16", 48, 768, 16), ("bf16", 256, 256, 16), ("bf16", 257, 136, 7),
          ("bf16", 4500, 72, 33), ("bf16", 9000, 264, 48), ("f32", 1, 4, 1), ("f32", 17, 68, 5), ("f32", 256, 256, 17),
-         ("f32", 300, 1028, 64), ("f32", 5000, 100, 20), ("f32", 16500, 64, 40)]
+         ("f32", 300, 1028, 64), ("f32", 5000, 100, 20), ("f32", 16500, 64, 40), ("f32", 4200, 516, 33),
+         ("f32", 700, 132, 64), ("f32", 33, 256, 63), ("bf16", 33, 64, 49)]
 
 
 @pytest.mark.parametrize("dtype,T,d,E", CASES)
