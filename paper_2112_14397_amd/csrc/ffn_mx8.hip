@@ -518,8 +518,9 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
 //     BIG                   -   23.4  25.1  44.0  84.1   276 /    -    445                     -   36.2  38.1  42.8  49.6   207 /   325
 //     BIG8                  -   21.8  23.9  40.8  77.2   256 /    -    420                     -   35.3  37.8  42.2  50.5   218 /   342
 //     few rows            16.4  25.1  62.9   157     -     - /  74.5     -                   17.9  28.1  65.9   162     -     - /     -
-// Few rows where no more than a pair falls to an expert and their weights are little (8 tokens, 16 pairs: 20 us for both, in tiles 29;
-// one token 13, 23), and for sizes that the tile kernel does not take.
+// Few rows for up to eight pairs of as many experts, whose weights are little (us for both products, few rows / tiles, d = 768, F = 3072:
+// 1 pair 13 / 16, 8 pairs 16 / 19, 16 pairs 21 / 20; d = 1024, F = 4096: 4 pairs 25 / 24, 8 pairs 32 / 25; d = 256, F = 1024: 64 pairs
+// 16 / 13), and for sizes that the tile kernel does not take.
 struct Big { static constexpr int BX = 256, BW = 256, WX = 2, WW = 2, NST = 2, WPE = 1, BLOCKS = 1; };
 struct Big8 { static constexpr int BX = 256, BW = 256, WX = 2, WW = 4, NST = 2, WPE = 2, BLOCKS = 1; };
 struct Mid { static constexpr int BX = 128, BW = 128, WX = 2, WW = 2, NST = 2, WPE = 2, BLOCKS = 2; };
@@ -532,7 +533,7 @@ struct Low { static constexpr int BX = 64, BW = 128, WX = 2, WW = 2, NST = 4, WP
 enum class Pick { FewRows, Sml, Mid, Slim, Low, Deep, Tall, Big, Big8 };
 Pick pick(const Ctx& c, const evomoe_shape& s, bool first) {
     const int64_t pairs = c.pair_hint > 0 && c.pair_hint < s.P_cap ? c.pair_hint : s.P_cap, weights = (int64_t)s.d * s.F;
-    if (s.d % 128 || s.F % 128 || (pairs <= s.E && pairs * weights <= 40000000)) return Pick::FewRows;
+    if (s.d % 128 || s.F % 128 || (pairs <= 8 && pairs <= s.E && pairs * weights <= 20000000)) return Pick::FewRows;
     // 256x256 tiles: an expert fills two of them, and there are enough (short contractions need more, their epilogues being long)
     const int n = first ? s.F : s.d;
     const int64_t tiles = ((pairs + 255) / 256 + s.E / 2) * ((n + 255) / 256);

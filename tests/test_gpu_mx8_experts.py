@@ -95,7 +95,7 @@ def ctx():
 
 
 # T, d, E, F, pairs, and the tiles of both products
-CASES = [(1, 32, 1, 32, 1, "32x32/4", "32x32/4"), (5, 64, 3, 96, 9, "32x32/4", "32x32/4"), (48, 768, 16, 1024, 16, "32x32/4", "32x32/4"),
+CASES = [(1, 32, 1, 32, 1, "32x32/4", "32x32/4"), (5, 64, 3, 96, 9, "32x32/4", "32x32/4"), (48, 768, 16, 1024, 8, "32x32/4", "32x32/4"), (48, 768, 16, 1024, 16, "64x128/4", "64x64/4"),
          (70, 160, 7, 288, 200, "32x32/4", "32x32/4"), (40, 1056, 5, 64, 90, "32x32/4", "32x32/4"),
          (33, 512, 33, 544, 33, "32x32/4", "32x32/4"), (300, 1184, 2, 32, 400, "32x32/4", "32x32/4"),
          (48, 768, 16, 1024, 48, "64x128/4", "64x64/4"), (300, 256, 4, 512, 700, "64x128/4", "64x128/4"),
