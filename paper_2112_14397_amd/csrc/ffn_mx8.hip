@@ -506,8 +506,8 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
 // (128x64 each, two to a SIMD): they fill each other's stalls in an epilogue that gelu and conversion make as long as the main loop.
 // MID: 128x128, two blocks per unit, one's epilogue under the other's products.  DEEP: 128x128 with four slabs on their way, for
 // long contractions with few tiles.  TALL: 192x128, three slabs, where DEEP's tiles begin another round on the CUs and TALL's do not.
-// SML: 64x128.  LOW: the same with four slabs, as long as its tiles are one round; SLIM: 64x64, for up to 16 rows an expert, where half as
-// many places would be in use.  us, E = 16, d = 768, F = 3072 (but for the last row) / E = 64, d = 1024, F = 4096:
+// SML: 64x128.  LOW: the same with four slabs, as long as its tiles are one round; SLIM: 64x64, where half as many places would be
+// in use.  us, E = 16, d = 768, F = 3072 (but for the last row) / E = 64, d = 1024, F = 4096:
 //   first product, pairs   48   512  2048  5998 16384 65536 /    96 65536    second product   48   512  2048  5998 16384 65536 / 65536
 //     SML                 13.0  14.4  20.6  40.6  96.2   359 /  48.5   575                   20.4  21.0  22.9  44.6  79.1   315 /   542
 //     MID                 14.8  16.2  21.9  37.0  79.9   281 /  52.6   467                   20.8  21.7  24.4  47.6  60.9   230 /   391
@@ -518,9 +518,12 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
 //     BIG                   -   23.4  25.1  44.0  84.1   276 /    -    445                     -   36.2  38.1  42.8  49.6   207 /   325
 //     BIG8                  -   21.8  23.9  40.8  77.2   256 /    -    420                     -   35.3  37.8  42.2  50.5   218 /   342
 //     few rows            16.4  25.1  62.9   157     -     - /  74.5     -                   17.9  28.1  65.9   162     -     - /     -
-// Few rows for up to eight pairs of as many experts, whose weights are little (us for both products, few rows / tiles, d = 768, F = 3072:
-// 1 pair 13 / 16, 8 pairs 16 / 19, 16 pairs 21 / 20; d = 1024, F = 4096: 4 pairs 25 / 24, 8 pairs 32 / 25; d = 256, F = 1024: 64 pairs
-// 16 / 13), and for sizes that the tile kernel does not take.
+// Few rows for up to eight pairs whose weights are little, and in the first product while its blocks of 32x32, each as long as the contraction,
+// are few (us, first product, few rows / SML: 8 pairs of 16 experts, d = 768, F = 3072 9.3 / 12.0, 16 pairs 13.2 / 12.5; 452 pairs of
+// one, d = 640, F = 768 8.7 / 10.6; 465 pairs of 40, d = 640, F = 640 11.7 / 9.3; 600 pairs of 4, d = 2048, F = 1024 22.4 / 15.8.
+// Second, few rows / SLIM: 1 pair, d = 768, F = 3072 10.2 / 11.1, 8 pairs 11.2 / 11.4; 1911 pairs of 32, d = 128, F = 3840 23.4 / 13.2),
+// and for sizes that the tile kernel does not take.  SLIM also while its tiles fill half of the CUs at most (the same 1911 pairs 13.2,
+// LOW 17.2; 452 pairs of one, d = 640 7.2, LOW 8.5).
 struct Big { static constexpr int BX = 256, BW = 256, WX = 2, WW = 2, NST = 2, WPE = 1, BLOCKS = 1; };
 struct Big8 { static constexpr int BX = 256, BW = 256, WX = 2, WW = 4, NST = 2, WPE = 2, BLOCKS = 1; };
 struct Mid { static constexpr int BX = 128, BW = 128, WX = 2, WW = 2, NST = 2, WPE = 2, BLOCKS = 2; };
@@ -533,13 +536,16 @@ struct Low { static constexpr int BX = 64, BW = 128, WX = 2, WW = 2, NST = 4, WP
 enum class Pick { FewRows, Sml, Mid, Slim, Low, Deep, Tall, Big, Big8 };
 Pick pick(const Ctx& c, const evomoe_shape& s, bool first) {
     const int64_t pairs = c.pair_hint > 0 && c.pair_hint < s.P_cap ? c.pair_hint : s.P_cap, weights = (int64_t)s.d * s.F;
-    if (s.d % 128 || s.F % 128 || (pairs <= 8 && pairs <= s.E && pairs * weights <= 20000000)) return Pick::FewRows;
+    if (s.d % 128 || s.F % 128) return Pick::FewRows;
+    const int64_t panels = (pairs + 31) / 32 + s.E / 2;       // of 32 rows; an expert's last one is half full
+    if (pairs <= 8 && pairs * weights <= 20000000) return Pick::FewRows;
+    if (first && (panels < pairs ? panels : pairs) * (s.F / 32) * s.d <= 400000) return Pick::FewRows;
     // 256x256 tiles: an expert fills two of them, and there are enough (short contractions need more, their epilogues being long)
     const int n = first ? s.F : s.d;
     const int64_t tiles = ((pairs + 255) / 256 + s.E / 2) * ((n + 255) / 256);
-    if (pairs >= 512 * s.E && tiles >= (first ? 2 * c.num_cu : c.num_cu / 2)) return first ? Pick::Big8 : Pick::Big;
+    if (n >= 256 && pairs >= 512 * s.E && tiles >= (first ? 2 * c.num_cu : c.num_cu / 2)) return first ? Pick::Big8 : Pick::Big;
     if (!first) {     // (a DEEP tile takes two thirds of a TALL one's time)
-        if (pairs <= 16 * s.E) return Pick::Slim;
+        if (pairs <= 16 * s.E || ((pairs + 63) / 64 + s.E / 2) * (n / 64) <= c.num_cu / 2) return Pick::Slim;
         auto rounds = [&](int64_t rows) { return (((pairs + rows - 1) / rows + s.E / 2) * ((n + 127) / 128) + c.num_cu - 1) / c.num_cu; };
         if (rounds(Low::BX) == 1) return Pick::Low;
         return 3 * rounds(Tall::BX) < 2 * rounds(Deep::BX) ? Pick::Tall : Pick::Deep;

@@ -95,14 +95,16 @@ def ctx():
 
 
 # T, d, E, F, pairs, and the tiles of both products
-CASES = [(1, 32, 1, 32, 1, "32x32/4", "32x32/4"), (5, 64, 3, 96, 9, "32x32/4", "32x32/4"), (48, 768, 16, 1024, 8, "32x32/4", "32x32/4"), (48, 768, 16, 1024, 16, "64x128/4", "64x64/4"),
+CASES = [(1, 32, 1, 32, 1, "32x32/4", "32x32/4"), (5, 64, 3, 96, 9, "32x32/4", "32x32/4"), (48, 768, 16, 1024, 8, "32x32/4", "32x32/4"), (48, 768, 16, 1024, 16, "32x32/4", "64x64/4"),
          (70, 160, 7, 288, 200, "32x32/4", "32x32/4"), (40, 1056, 5, 64, 90, "32x32/4", "32x32/4"),
          (33, 512, 33, 544, 33, "32x32/4", "32x32/4"), (300, 1184, 2, 32, 400, "32x32/4", "32x32/4"),
-         (48, 768, 16, 1024, 48, "64x128/4", "64x64/4"), (300, 256, 4, 512, 700, "64x128/4", "64x128/4"),
-         (90, 128, 64, 128, 400, "64x128/4", "64x64/4"), (60, 384, 5, 640, 77, "64x128/4", "64x64/4"),
-         (600, 128, 2, 256, 1500, "128x128/4", "64x128/4"), (500, 640, 3, 384, 1100, "128x128/4", "64x128/4"),
-         (100, 512, 1, 1152, 333, "128x128/4", "64x128/4"), (400, 768, 16, 256, 4000, "64x128/4", "128x128/4"),
-         (500, 1024, 8, 640, 3000, "128x128/4", "128x128/4"), (30, 256, 33, 896, 500, "64x128/4", "64x64/4")]
+         (48, 768, 16, 1024, 48, "32x32/4", "64x64/4"), (300, 256, 4, 512, 700, "32x32/4", "64x64/4"),
+         (90, 128, 64, 128, 400, "32x32/4", "64x64/4"), (60, 384, 5, 640, 77, "32x32/4", "64x64/4"),
+         (600, 128, 2, 256, 1500, "32x32/4", "64x64/4"), (500, 640, 3, 384, 1100, "32x32/4", "64x128/4"),
+         (100, 512, 1, 1152, 333, "32x32/4", "64x64/4"), (400, 768, 16, 256, 4000, "64x128/4", "128x128/4"),
+         (500, 1024, 8, 640, 3000, "128x128/4", "128x128/4"), (30, 256, 33, 896, 500, "32x32/4", "64x64/4"),
+         (300, 512, 4, 1152, 700, "64x128/4", "64x64/4"), (64, 256, 16, 2816, 300, "64x128/4", "64x64/4"),
+         (700, 640, 2, 1280, 1100, "128x128/4", "64x128/4"), (700, 384, 2, 1280, 1300, "128x128/4", "64x128/4")]
 # ... where the oracle looks at some rows
 LARGE = [(500, 128, 2, 4352, 8100, "256x256/8", "64x128/4"), (400, 384, 1, 8832, 4000, "256x256/8", "64x128/4"),
          (700, 1024, 3, 128, 8200, "128x128/4", "256x256/4"), (300, 4480, 2, 256, 2600, "128x128/4", "256x256/4"),
