@@ -154,6 +154,151 @@ __global__ __launch_bounds__(256) void mx8_few_rows_kernel(Mx8Args p)
     }
 }
 
+// Any multiples of 32 for K and N, many rows: tiles of 128x128, four waves of 64x64, through registers into the LDS, one slab of 128 k's
+// ahead, two blocks to a CU.  What lies beyond K is 0 with a scale of 1; columns beyond N repeat the last ones and are not stored.  Scales are read
+// byte by byte, as a row of them begins anywhere.  The LDS layout is the tile kernel's (below).
+template <int EPI>
+__global__ __launch_bounds__(256, 2) void mx8_any_size_kernel(Mx8Args p)
+{
+    constexpr bool FIRST = EPI != TO_OUTPUT;
+    __shared__ __align__(16) unsigned char data[2][256 * 128];           // 128 rows of X, then 128 of W
+    __shared__ uint32_t scales[2][256];
+    const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wx = wave >> 1, ww = wave & 1;
+    // lane e: expert e's rows, and the row tiles up to it
+    const int begin = clamp_pairs(p.expert_offsets[min(lane, p.E)], p.P_cap),
+              end = clamp_pairs(p.expert_offsets[min(lane + 1, p.E)], p.P_cap);
+    int upto = (end - begin + 127) / 128;
+    const int mine = upto;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(upto, o, 64);
+        if (lane >= o) upto += v;
+    }
+    const int kg = p.K / kMxGroup, nct = (p.N + 127) / 128, nslab = (p.K + 127) / 128;
+    const int64_t tiles = (int64_t)__builtin_amdgcn_readlane(upto, 63) * nct;
+    for (int64_t at = blockIdx.x; at < tiles; at += gridDim.x) {
+        const int tile = (int)(at / nct), n0 = (int)(at - (int64_t)tile * nct) * 128, g = __popcll(__ballot(upto <= tile));
+        const int row0 = __builtin_amdgcn_readlane(begin, g) + (tile - __builtin_amdgcn_readlane(upto - mine, g)) * 128;
+        const int rows = min(128, __builtin_amdgcn_readlane(end, g) - row0);
+        auto x_row = [&](int r) {
+            const int at_row = row0 + min(r, rows - 1);
+            return (int64_t)(p.rows ? p.rows[at_row] : at_row);
+        };
+        auto w_row = [&](int r) { return (int64_t)g * p.N + min(n0 + r, p.N - 1); };
+        // this thread's part of a slab: chunk c16 of the rows r8, r8 + 32, .. of X and of W, and the scales of one row
+        const int r8 = threadIdx.x >> 3, c16 = threadIdx.x & 7, sr = threadIdx.x & 127;
+        const uint8_t* from[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            from[i] = p.X + x_row(r8 + 32 * i) * p.K;
+            from[4 + i] = p.W + w_row(r8 + 32 * i) * p.K;
+        }
+        const uint8_t* scale_from = threadIdx.x < 128 ? p.Xs + x_row(sr) * kg : p.Ws + w_row(sr) * kg;
+        u32x4 next[8];
+        uint32_t next_scale;
+        auto load = [&](int s) {
+            const int k = s * 128 + c16 * 16;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) next[i] = k < p.K ? *reinterpret_cast<const u32x4*>(from[i] + k) : u32x4{0u, 0u, 0u, 0u};
+            next_scale = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) next_scale |= (uint32_t)(s * 4 + j < kg ? scale_from[s * 4 + j] : 127) << (8 * j);
+        };
+        auto put = [&](int s) {
+            unsigned char* to = data[s & 1];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = r8 + 32 * (i & 3);
+                *reinterpret_cast<u32x4*>(to + ((i >> 2) * 128 + r) * 128 + ((c16 ^ (r >> 1 & 7)) << 4)) = next[i];
+            }
+            scales[s & 1][threadIdx.x] = next_scale;
+        };
+        f32x16 acc[2][2] = {};
+        load(0);
+        put(0);
+        __syncthreads();
+        for (int s = 0; s < nslab; ++s) {
+            if (s + 1 < nslab) load(s + 1);
+            const unsigned char* st = data[s & 1];
+            const uint32_t* sc = scales[s & 1];
+            const int key = l32 >> 1 & 7;
+            auto fragment = [&](int row, int ks) {
+                const u32x4 lo = *reinterpret_cast<const u32x4*>(st + row * 128 + (((ks * 4 + half) ^ key) << 4));
+                const u32x4 hi = *reinterpret_cast<const u32x4*>(st + row * 128 + (((ks * 4 + 2 + half) ^ key) << 4));
+                return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+            };
+            int sx[2], sw[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                sx[i] = (int)(sc[(wx * 2 + i) * 32 + l32] >> (8 * half));
+                sw[i] = (int)(sc[128 + (ww * 2 + i) * 32 + l32] >> (8 * half));
+            }
+            auto kstep = [&](auto op, int ks) {
+                i32x8 x[2], w[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    x[i] = fragment((wx * 2 + i) * 32 + l32, ks);
+                    w[i] = fragment(128 + (ww * 2 + i) * 32 + l32, ks);
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[i][j] = mfma32<decltype(op)::value>(w[i], x[j], acc[i][j], sw[i], sx[j]);
+            };
+            kstep(std::integral_constant<int, 0>{}, 0);
+            kstep(std::integral_constant<int, 2>{}, 1);
+            if (s + 1 < nslab) put(s + 1);           // (its last readers passed the barrier before this slab)
+            __syncthreads();
+        }
+        // lane = row, registers = columns, as in the tile kernel
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int n = n0 + (ww * 2 + i) * 32;                    // N is a multiple of 32
+            const uint32_t beyond = n < p.N ? 0u : 0x40000000u;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int r0 = (wx * 2 + j) * 32, there = min(32, max(0, rows - r0));
+                const int64_t first = (int64_t)(row0 + r0);
+                asm volatile("" : "+v"(acc[i][j]));
+                float v[16];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x4 b = p.bias && n < p.N ? *reinterpret_cast<const f32x4*>(p.bias + (int64_t)g * p.N + n + 8 * q + 4 * half) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v[4 * q + r] = acc[i][j][4 * q + r] + b[r];
+                }
+                if constexpr (FIRST) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) v[r] = EPI == TO_RELU ? relu(v[r]) : gelu5(v[r]);
+                    uint32_t ma = __float_as_uint(mx_max(v)), mb = ma;
+                    swap_halves(ma, mb);
+                    const uint32_t b = mx_scale_byte(fmaxf(__uint_as_float(ma), __uint_as_float(mb)));
+                    uint32_t d[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) d[q] = mx_pack4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3], b);
+                    swap_halves(d[0], d[2]);
+                    swap_halves(d[1], d[3]);
+                    __builtin_amdgcn_raw_buffer_store_b128(u32x4{d[0], d[2], d[1], d[3]}, rows_of(p.Aq + first * p.N, there * p.N),
+                                                           (l32 * p.N + n + 16 * half) | beyond, 0, 0);
+                    const int ng = p.N / kMxGroup;
+                    __builtin_amdgcn_raw_buffer_store_b8((uint8_t)b, rows_of(p.As + first * ng, there * ng),
+                                                         half ? 0x40000000 : (int)((l32 * ng + n / kMxGroup) | beyond), 0, 0);
+                } else {
+                    uint32_t d[8];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) d[q] = pack_bf16x2(v[2 * q], v[2 * q + 1]);
+                    swap_halves(d[0], d[4]); swap_halves(d[1], d[5]); swap_halves(d[2], d[6]); swap_halves(d[3], d[7]);
+                    const auto to = rows_of(p.O + first * p.N, there * p.N * 2);
+                    const uint32_t off = ((l32 * p.N + n + 16 * half) * 2) | beyond;
+                    __builtin_amdgcn_raw_buffer_store_b128(u32x4{d[0], d[1], d[4], d[5]}, to, off, 0, 0);
+                    __builtin_amdgcn_raw_buffer_store_b128(u32x4{d[2], d[3], d[6], d[7]}, to, off + 16, 0, 0);
+                }
+            }
+        }
+    }
+}
+
 // The tile kernel, for d and F that are multiples of 128.  A block of WX x WW waves computes BX rows of X by BW rows of W, a
 // wave TX x TW matrix instructions of 32 x 32.  The contraction runs in slabs of 128 bytes (one line of every row), two LDS stages
 // deep; a stage holds both operands' slabs, rows of 128 bytes with the 16-byte chunk c of row r at chunk c ^ (r >> 1 & 7), so that
@@ -522,7 +667,9 @@ __global__ __launch_bounds__(WX * WW * 64, WPE) void mx8_tile_kernel(Mx8Args p, 
 // are few (us, first product, few rows / SML: 8 pairs of 16 experts, d = 768, F = 3072 9.3 / 12.0, 16 pairs 13.2 / 12.5; 452 pairs of
 // one, d = 640, F = 768 8.7 / 10.6; 465 pairs of 40, d = 640, F = 640 11.7 / 9.3; 600 pairs of 4, d = 2048, F = 1024 22.4 / 15.8.
 // Second, few rows / SLIM: 1 pair, d = 768, F = 3072 10.2 / 11.1, 8 pairs 11.2 / 11.4; 1911 pairs of 32, d = 128, F = 3840 23.4 / 13.2),
-// and for sizes that the tile kernel does not take.  SLIM also while its tiles fill half of the CUs at most (the same 1911 pairs 13.2,
+// and for sizes that the tile kernel does not take, until the kernel of any size is faster (us, few rows / any size, both products: 48 pairs
+// of 16 experts, d = 800, F = 2400 24 / 53; 2000 pairs, d = 736, F = 2080 71 / 58; 8000 pairs, d = 992, F = 3104 423 / 208; 32768 pairs of
+// 64, d = 352, F = 1376 337 / 156).  SLIM also while its tiles fill half of the CUs at most (the same 1911 pairs 13.2,
 // LOW 17.2; 452 pairs of one, d = 640 7.2, LOW 8.5).
 struct Big { static constexpr int BX = 256, BW = 256, WX = 2, WW = 2, NST = 2, WPE = 1, BLOCKS = 1; };
 struct Big8 { static constexpr int BX = 256, BW = 256, WX = 2, WW = 4, NST = 2, WPE = 2, BLOCKS = 1; };
@@ -533,15 +680,19 @@ struct Tall { static constexpr int BX = 192, BW = 128, WX = 2, WW = 2, NST = 3, 
 struct Slim { static constexpr int BX = 64, BW = 64, WX = 2, WW = 2, NST = 4, WPE = 2, BLOCKS = 2; };
 struct Low { static constexpr int BX = 64, BW = 128, WX = 2, WW = 2, NST = 4, WPE = 1, BLOCKS = 1; };
 
-enum class Pick { FewRows, Sml, Mid, Slim, Low, Deep, Tall, Big, Big8 };
+enum class Pick { FewRows, AnySize, Sml, Mid, Slim, Low, Deep, Tall, Big, Big8 };
 Pick pick(const Ctx& c, const evomoe_shape& s, bool first) {
     const int64_t pairs = c.pair_hint > 0 && c.pair_hint < s.P_cap ? c.pair_hint : s.P_cap, weights = (int64_t)s.d * s.F;
-    if (s.d % 128 || s.F % 128) return Pick::FewRows;
-    const int64_t panels = (pairs + 31) / 32 + s.E / 2;       // of 32 rows; an expert's last one is half full
-    if (pairs <= 8 && pairs * weights <= 20000000) return Pick::FewRows;
-    if (first && (panels < pairs ? panels : pairs) * (s.F / 32) * s.d <= 400000) return Pick::FewRows;
-    // 256x256 tiles: an expert fills two of them, and there are enough (short contractions need more, their epilogues being long)
     const int n = first ? s.F : s.d;
+    // tiles of few rows: an expert's last 32 rows are half full, and there are no more of them than pairs
+    const int64_t panels = (pairs + 31) / 32 + s.E / 2, few = (panels < pairs ? panels : pairs) * (n / 32);
+    if (s.d % 128 || s.F % 128) {     // a tile of any size costs as much as four of few rows, and eight of those per CU as much as a round of it
+        const int64_t any = ((pairs + 127) / 128 + s.E / 2) * ((n + 127) / 128);
+        return few <= 8 * c.num_cu || few <= 4 * any ? Pick::FewRows : Pick::AnySize;
+    }
+    if (pairs <= 8 && pairs * weights <= 20000000) return Pick::FewRows;
+    if (first && few * s.d <= 400000) return Pick::FewRows;
+    // 256x256 tiles: an expert fills two of them, and there are enough (short contractions need more, their epilogues being long)
     const int64_t tiles = ((pairs + 255) / 256 + s.E / 2) * ((n + 255) / 256);
     if (n >= 256 && pairs >= 512 * s.E && tiles >= (first ? 2 * c.num_cu : c.num_cu / 2)) return first ? Pick::Big8 : Pick::Big;
     if (!first) {     // (a DEEP tile takes two thirds of a TALL one's time)
@@ -581,9 +732,16 @@ template <int EPI> hipError_t launch_few_rows(const Ctx& c, const evomoe_shape& 
     return hipGetLastError();
 }
 
+template <int EPI> hipError_t launch_any_size(const Ctx& c, const evomoe_shape& s, const Mx8Args& a) {
+    const int64_t worst = ((s.P_cap + 127) / 128 + s.E) * ((a.N + 127) / 128), cap = (int64_t)c.num_cu * 2;
+    hipLaunchKernelGGL(mx8_any_size_kernel<EPI>, dim3((unsigned)(worst < cap ? worst : cap)), dim3(256), 0, c.stream, a);
+    return hipGetLastError();
+}
+
 template <int EPI> hipError_t launch_first(const Ctx& c, const evomoe_shape& s, const Mx8Args& a) {
     switch (pick(c, s, true)) {
         case Pick::FewRows: return launch_few_rows<EPI>(c, s, a);
+        case Pick::AnySize: return launch_any_size<EPI>(c, s, a);
         case Pick::Sml: return launch_tiles<EPI, Sml>(c, s, a);
         case Pick::Mid: return launch_tiles<EPI, Mid>(c, s, a);
         default: return launch_tiles<EPI, Big8>(c, s, a);
@@ -592,6 +750,7 @@ template <int EPI> hipError_t launch_first(const Ctx& c, const evomoe_shape& s, 
 hipError_t launch_second(const Ctx& c, const evomoe_shape& s, const Mx8Args& a) {
     switch (pick(c, s, false)) {
         case Pick::FewRows: return launch_few_rows<TO_OUTPUT>(c, s, a);
+        case Pick::AnySize: return launch_any_size<TO_OUTPUT>(c, s, a);
         case Pick::Deep: return launch_tiles<TO_OUTPUT, Deep>(c, s, a);
         case Pick::Slim: return launch_tiles<TO_OUTPUT, Slim>(c, s, a);
         case Pick::Low: return launch_tiles<TO_OUTPUT, Low>(c, s, a);
@@ -607,6 +766,7 @@ size_t aq_bytes(const evomoe_shape& s) { return ((size_t)s.P_cap * s.F + 255) & 
 FfnTile mx8_ffn_tile(const Ctx& c, const evomoe_shape& s, int kernel) {
     switch (pick(c, s, kernel == EVOMOE_K_FFN_MX8_GEMM1)) {
         case Pick::FewRows: return {32, 32, 4};
+        case Pick::AnySize: return {128, 128, 4};
         case Pick::Sml: return {Sml::BX, Sml::BW, 4};
         case Pick::Mid: return {Mid::BX, Mid::BW, 4};
         case Pick::Deep: return {Deep::BX, Deep::BW, 4};

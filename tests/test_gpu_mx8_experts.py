@@ -104,7 +104,9 @@ CASES = [(1, 32, 1, 32, 1, "32x32/4", "32x32/4"), (5, 64, 3, 96, 9, "32x32/4", "
          (100, 512, 1, 1152, 333, "32x32/4", "64x64/4"), (400, 768, 16, 256, 4000, "64x128/4", "128x128/4"),
          (500, 1024, 8, 640, 3000, "128x128/4", "128x128/4"), (30, 256, 33, 896, 500, "32x32/4", "64x64/4"),
          (300, 512, 4, 1152, 700, "64x128/4", "64x64/4"), (64, 256, 16, 2816, 300, "64x128/4", "64x64/4"),
-         (700, 640, 2, 1280, 1100, "128x128/4", "64x128/4"), (700, 384, 2, 1280, 1300, "128x128/4", "64x128/4")]
+         (700, 640, 2, 1280, 1100, "128x128/4", "64x128/4"), (700, 384, 2, 1280, 1300, "128x128/4", "64x128/4"),
+         (500, 160, 3, 1120, 4000, "128x128/4", "32x32/4"), (300, 1120, 3, 96, 4000, "32x32/4", "128x128/4"),
+         (300, 1056, 5, 1184, 3000, "128x128/4", "128x128/4"), (200, 32, 2, 2080, 3000, "128x128/4", "32x32/4")]
 # ... where the oracle looks at some rows
 LARGE = [(500, 128, 2, 4352, 8100, "256x256/8", "64x128/4"), (400, 384, 1, 8832, 4000, "256x256/8", "64x128/4"),
          (700, 1024, 3, 128, 8200, "128x128/4", "256x256/4"), (300, 4480, 2, 256, 2600, "128x128/4", "256x256/4"),
