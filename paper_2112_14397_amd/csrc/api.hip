@@ -75,11 +75,12 @@ evomoe_status check_topk(const evomoe_topk* o, int E) {
         evomoe_status st_ = check_shape(shape);            \
         if (st_ != EVOMOE_OK) return st_;                  \
     } while (0)
-// ... and for the operators beside the DTS gate, whose kernels step over tokens with 32-bit counters
+// ... and for the operators beside the DTS gate, whose kernels step over tokens and columns with 32-bit counters, and whose grids have up
+// to four threads a token
 #define CHECK_CTX_BLOCK()                                           \
     do {                                                            \
         CHECK_CTX_SHAPE();                                          \
-        if (shape->T > (1 << 30)) return EVOMOE_EUNSUPPORTED;       \
+        if (shape->T > (1 << 29) || shape->d > (1 << 30)) return EVOMOE_EUNSUPPORTED; \
     } while (0)
 
 evomoe_status from_hip(hipError_t e) { return e == hipSuccess ? EVOMOE_OK : EVOMOE_EHIP; }

@@ -78,7 +78,8 @@ def test_null_and_misaligned_arguments(name):
 @pytest.mark.parametrize("bad,status", [(dict(T=0), B.EVOMOE_EINVAL), (dict(d=-64), B.EVOMOE_EINVAL), (dict(E=0), B.EVOMOE_EINVAL),
                                         (dict(P=0), B.EVOMOE_EINVAL), (dict(E=65), B.EVOMOE_EUNSUPPORTED),
                                         (dict(d=68), B.EVOMOE_EUNSUPPORTED), (dict(T=1 << 29), B.EVOMOE_EUNSUPPORTED),
-                                        (dict(T=(1 << 30) + 1, E=1), B.EVOMOE_EUNSUPPORTED)])
+                                        (dict(T=(1 << 29) + 1, E=1), B.EVOMOE_EUNSUPPORTED),
+                                        (dict(T=1, d=(1 << 30) + 64), B.EVOMOE_EUNSUPPORTED)])
 def test_shapes(name, bad, status):
     assert call(name, shape(**bad), marshalled(GOOD[name])) == status
 
