@@ -283,7 +283,7 @@ evomoe_status evomoe_diversify(evomoe_ctx* ctx, const evomoe_shape* shape,
  * the calls below are the ones that the DTS-gate path has no part of.  They take the same shape, context and
  * conventions (with T up to 2^29 and d up to 2^30), and their outputs are the inputs of evomoe_dispatch, evomoe_expert_ffn, evomoe_combine and
  * evomoe_balance_loss.  They run on the context's device whatever device is current, allocate nothing (but for
- * evomoe_gate_logits, whose split copy of W_g grows with d as evomoe_dts_gate's) and may be captured into a HIP graph;
+ * evomoe_gate_logits of a bf16 layer's more than 4096 tokens, whose split copy of W_g grows with d as evomoe_dts_gate's) and may be captured into a HIP graph;
  * calls that may overlap in time need contexts and workspaces of their own. */
 
 /* Gate logits:  logits[t,:] = x_t . W_g + b_g.

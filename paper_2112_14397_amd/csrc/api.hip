@@ -437,7 +437,7 @@ evomoe_status evomoe_gate_logits(evomoe_ctx* ctx, const evomoe_shape* shape, con
     CHECK_CTX_BLOCK();
     REQUIRE_PTR(x); REQUIRE_PTR(Wg); REQUIRE_PTR(logits); OPTIONAL_PTR(bg);
     ON_DEVICE();
-    if (shape->dtype == EVOMOE_BF16) {
+    if (gate_logits_use_planes(ctx->c, *shape)) {
         evomoe_status st = ensure_wg_planes(ctx->c, (size_t)3 * 64 * ((shape->d + 31) / 32 * 32) * sizeof(uint16_t));
         if (st != EVOMOE_OK) return st;
     }

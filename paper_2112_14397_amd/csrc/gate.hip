@@ -579,6 +579,8 @@ static hipError_t logits_launch(const Ctx& c, const evomoe_shape& s, const void*
         default: return with(std::integral_constant<int, 4>{});
     }
 }
+bool gate_logits_use_planes(const Ctx& c, const evomoe_shape& s) { return s.dtype == EVOMOE_BF16 && !few_logits(c, s); }
+
 hipError_t launch_gate_logits(const Ctx& c, const evomoe_shape& s, const void* x, const float* Wg, const float* bg,
                               float* logits) {
     return s.dtype == EVOMOE_BF16 ? logits_launch<bf16_t>(c, s, x, Wg, bg, logits)

@@ -15,6 +15,7 @@ hipError_t launch_dts_gate_bwd(const Ctx& c, const evomoe_shape& s, const float*
                                float* dWg, float* dbg, void* dx, void* workspace,
                                const float* dgprime_coef = nullptr, float coef_scale = 0.f);
 size_t gate_bwd_workspace_bytes(const evomoe_shape& s);
+bool gate_logits_use_planes(const Ctx& c, const evomoe_shape& s);      // whether launch_gate_logits needs the split copy of W_g
 hipError_t launch_gate_logits(const Ctx& c, const evomoe_shape& s, const void* x, const float* Wg, const float* bg,
                               float* logits);
 // part: gate_bwd_workspace_bytes(s) hold it

@@ -103,3 +103,27 @@ def test_a_captured_pass_outlives_a_larger_one():
         torch.cuda.synchronize()
         ctx.close()
         mine.close()
+
+
+def test_few_tokens_captured_before_any_other_call():
+    """Up to 4096 tokens nothing is allocated, so that the first call of a context may be a captured one."""
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        g = torch.Generator(device="cuda").manual_seed(4)
+        new = lambda *s: torch.randn(*s, generator=g, device="cuda")
+        T, d, E = 48, 4096, 16
+        shape, x, W, z = B.make_shape(T, d, E, d, "bf16", "gelu", 1), new(T, d).bfloat16(), new(d, E), new(T, E)
+        other, want = B.Context(), torch.empty(T, E, device="cuda")
+        B.evomoe_gate_logits(other, shape, x, W, None, want)
+        ctx = B.Context()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            B.evomoe_gate_logits(ctx, shape, x, W, None, z)
+        for _ in range(3):
+            z.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(z, want)
+        ctx.close()
+        other.close()
