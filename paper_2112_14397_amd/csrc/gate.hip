@@ -7,6 +7,7 @@
 // (integer atomics into counts[E] and, if asked for, into the per-256-token histograms the dispatch
 // starts from; both are cleared by gate_prep_kernel right before, or, where one block of 1024 threads works on all
 // tokens, written by it outright).
+#include <algorithm>
 #include <type_traits>
 
 #include "kernels.h"
@@ -767,7 +768,7 @@ __device__ __forceinline__ bf16x8 lds_read_tr(const unsigned char* q, int row_by
 template <int KE, int NE>
 __global__ __launch_bounds__(256, 2) void gate_bwd_mfma_kernel(
     const float* __restrict__ dz, const bf16_t* __restrict__ x, const float* __restrict__ Wg, int T, int d, int E,
-    int tokens_per_block, const bf16_t* dx_in, bf16_t* dx, float* __restrict__ dWg_part, float* __restrict__ dbg_part)
+    int tokens_per_block, int slice0, const bf16_t* dx_in, bf16_t* dx, float* __restrict__ dWg_part, float* __restrict__ dbg_part)
 {
     constexpr int EPL = 32 * NE;                     // experts per LDS row (zero beyond E)
     constexpr int DZN = kGbTok * EPL / 256;          // dz values per thread and chunk
@@ -779,7 +780,7 @@ __global__ __launch_bounds__(256, 2) void gate_bwd_mfma_kernel(
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int l32 = lane & 31, kg = lane >> 5, s16 = lane & 15, half = (lane >> 4) & 1;
-    const int blk = blockIdx.x, slice = blockIdx.y;
+    const int blk = blockIdx.x, slice = slice0 + blockIdx.y;
     const int c0 = slice * kGbCols + wave * 64;      // this wave's first column
     const int s_begin = blk * tokens_per_block, s_end = min(T, s_begin + tokens_per_block);
     const int nch = (s_end - s_begin + kGbTok - 1) / kGbTok;
@@ -965,12 +966,12 @@ LbPlan logits_bwd_f32_plan(const evomoe_shape& s) {
 template <int NE>
 __global__ __launch_bounds__(256) void logits_bwd_f32_kernel(
     const float* __restrict__ dz, const float* __restrict__ x, const float* __restrict__ Wg, int T, int d, int E, int tokens_per_block,
-    const float* dx_in, float* dx, float* __restrict__ dWg_part, float* __restrict__ dbg_part)
+    int slice0, const float* dx_in, float* dx, float* __restrict__ dWg_part, float* __restrict__ dbg_part)
 {
     constexpr int LD = 32 * NE + 1, DZN = 32 * 32 * NE / 256;
     __shared__ float sdz[32 * LD];                   // [token][expert], zero beyond
     const int tid = threadIdx.x, lane = tid & 63, i32 = lane & 31, h = lane >> 5;
-    const int col = blockIdx.y * 128 + (tid >> 6) * 32 + i32;
+    const int slice = slice0 + blockIdx.y, col = slice * 128 + (tid >> 6) * 32 + i32;
     const bool col_ok = col < d;
     const int s_begin = blockIdx.x * tokens_per_block, s_end = min(T, s_begin + tokens_per_block);
 
@@ -1014,7 +1015,7 @@ __global__ __launch_bounds__(256) void logits_bwd_f32_kernel(
         for (int r = 0; r < 16; ++r) { acc_x[r] = in[r]; xc[r] = xv[r]; }
         __syncthreads();
         if (s0 + 32 < s_end) load(s0 + 32);
-        if (blockIdx.y == 0 && tid < E)
+        if (slice == 0 && tid < E)
             for (int t = 0; t < 32; ++t) sb += sdz[t * LD + tid];
 #pragma unroll
         for (int k = 0; k < 16; ++k)
@@ -1036,11 +1037,11 @@ __global__ __launch_bounds__(256) void logits_bwd_f32_kernel(
         asm volatile("" : "+v"(acc_w[n]));
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            const int k = blockIdx.y * 128 + (tid >> 6) * 32 + 8 * (r >> 2) + 4 * h + (r & 3), e = n * 32 + i32;
+            const int k = slice * 128 + (tid >> 6) * 32 + 8 * (r >> 2) + 4 * h + (r & 3), e = n * 32 + i32;
             if (k < d && e < E) dWg_part[((size_t)blockIdx.x * (d + 1) + k) * E + e] = acc_w[n][r];
         }
     }
-    if (blockIdx.y == 0 && tid < E) dbg_part[(size_t)blockIdx.x * (d + 1) * E + tid] = sb;
+    if (slice == 0 && tid < E) dbg_part[(size_t)blockIdx.x * (d + 1) * E + tid] = sb;
 }
 
 bool gate_bwd_use_mfma(const evomoe_shape& s) { return s.dtype == EVOMOE_BF16; }   // (d is a multiple of 8 there)
@@ -1049,7 +1050,9 @@ bool gate_bwd_use_mfma(const evomoe_shape& s) { return s.dtype == EVOMOE_BF16; }
 
 // out[i] = sum over chunks of part[chunk][i], i < n0 + n1; the first n0 sums go to out0, the rest to out1 (or
 // nowhere if out1 is null).  Four thread groups take a quarter of the chunks each (ascending, 16 independent loads
-// in flight), then the four partial sums are added in group order.  Fixed order: reproducible.
+// in flight), then the four partial sums are added in group order.  Fixed order: reproducible.  A block has 64 elements at a time: a
+// block for every 64 up to kSumBlocks blocks (a grid dimension holds fewer than 2^32 threads, and tables may have more than 2^30 elements).
+constexpr size_t kSumBlocks = (size_t)1 << 20;
 __global__ __launch_bounds__(256) void sum_chunks_kernel(const float* __restrict__ part, int nchunk, size_t n0,
                                                          size_t n1, float* __restrict__ out0,
                                                          float* __restrict__ out1)
@@ -1057,25 +1060,28 @@ __global__ __launch_bounds__(256) void sum_chunks_kernel(const float* __restrict
     __shared__ float red[4][64];
     const int o = threadIdx.x & 63, gq = threadIdx.x >> 6;
     const size_t n = n0 + n1;
-    const size_t i = (size_t)blockIdx.x * 64 + o;
     const int per = (nchunk + 3) / 4;
     const int c_lo = gq * per, c_hi = min(nchunk, c_lo + per);
-    float s = 0.f;
-    if (i < n) {
-        for (int c0 = c_lo; c0 < c_hi; c0 += 16) {
-            float v[16];
+    for (size_t i0 = (size_t)blockIdx.x * 64; i0 < n; i0 += (size_t)gridDim.x * 64) {
+        const size_t i = i0 + o;
+        float s = 0.f;
+        if (i < n) {
+            for (int c0 = c_lo; c0 < c_hi; c0 += 16) {
+                float v[16];
 #pragma unroll
-            for (int u = 0; u < 16; ++u) v[u] = (c0 + u < c_hi) ? part[(size_t)(c0 + u) * n + i] : 0.f;
+                for (int u = 0; u < 16; ++u) v[u] = (c0 + u < c_hi) ? part[(size_t)(c0 + u) * n + i] : 0.f;
 #pragma unroll
-            for (int u = 0; u < 16; ++u) s += v[u];
+                for (int u = 0; u < 16; ++u) s += v[u];
+            }
         }
-    }
-    red[gq][o] = s;
-    __syncthreads();
-    if (gq == 0 && i < n) {
-        const float r = ((red[0][o] + red[1][o]) + red[2][o]) + red[3][o];
-        if (i < n0) out0[i] = r;
-        else if (out1) out1[i - n0] = r;
+        red[gq][o] = s;
+        __syncthreads();
+        if (gq == 0 && i < n) {
+            const float r = ((red[0][o] + red[1][o]) + red[2][o]) + red[3][o];
+            if (i < n0) out0[i] = r;
+            else if (out1) out1[i - n0] = r;
+        }
+        __syncthreads();                             // (the sums have been read)
     }
 }
 
@@ -1121,6 +1127,7 @@ static hipError_t gate_bwd_t(const Ctx& c, const evomoe_shape& s, const float* d
     return hipGetLastError();
 }
 
+constexpr int kSlicesPerLaunch = 32768;
 // part: chunk c's partial sums, [dWg partial: d x E][dbg partial: E], contiguous
 static hipError_t gate_bwd_contract(const Ctx& c, const evomoe_shape& s, const float* dz, const void* x, const float* Wg,
                                     const void* dx_in, float* dWg, float* dbg, void* dx, float* part, bool logits) {
@@ -1133,22 +1140,25 @@ static hipError_t gate_bwd_contract(const Ctx& c, const evomoe_shape& s, const f
     hipError_t err;
     {
         ProfScope ps(c, EVOMOE_K_GATE_BWD_MAIN);
-        if (mfma) {
-            const dim3 grid(plan.nblk, plan.slices);
+        if (mfma || logits) {
+            // (a grid has up to 65536 blocks in its second dimension: wider layers take several launches)
+            const int slices = mfma ? plan.slices : lplan.slices;
+            for (int y = 0; y < slices; y += kSlicesPerLaunch) {
+                const dim3 grid(nchunk, std::min(slices - y, kSlicesPerLaunch));
 #define EVOMOE_GBM(KEV, NEV)                                                                             \
     hipLaunchKernelGGL((gate_bwd_mfma_kernel<KEV, NEV>), grid, dim3(256), 0, c.stream, dz, (const bf16_t*)x, Wg, \
-                       s.T, s.d, s.E, plan.tokens_per_block, (const bf16_t*)dx_in, (bf16_t*)dx, part, dbg_part)
-            if (s.E <= 16) EVOMOE_GBM(1, 1);
-            else if (s.E <= 32) EVOMOE_GBM(2, 1);
-            else if (s.E <= 48) EVOMOE_GBM(3, 2);
-            else EVOMOE_GBM(4, 2);
+                       s.T, s.d, s.E, plan.tokens_per_block, y, (const bf16_t*)dx_in, (bf16_t*)dx, part, dbg_part)
+                if (!mfma) {
+                    auto kern = s.E <= 32 ? logits_bwd_f32_kernel<1> : logits_bwd_f32_kernel<2>;
+                    hipLaunchKernelGGL(kern, grid, dim3(256), 0, c.stream, dz, (const float*)x, Wg, s.T, s.d, s.E, lplan.tokens_per_block, y,
+                                       (const float*)dx_in, (float*)dx, part, dbg_part);
+                } else if (s.E <= 16) EVOMOE_GBM(1, 1);
+                else if (s.E <= 32) EVOMOE_GBM(2, 1);
+                else if (s.E <= 48) EVOMOE_GBM(3, 2);
+                else EVOMOE_GBM(4, 2);
 #undef EVOMOE_GBM
-            err = hipGetLastError();
-        } else if (logits) {
-            auto kern = s.E <= 32 ? logits_bwd_f32_kernel<1> : logits_bwd_f32_kernel<2>;
-            hipLaunchKernelGGL(kern, dim3(lplan.nblk, lplan.slices), dim3(256), 0, c.stream, dz, (const float*)x, Wg, s.T, s.d, s.E,
-                               lplan.tokens_per_block, (const float*)dx_in, (float*)dx, part, dbg_part);
-            err = hipGetLastError();
+                if (err = hipGetLastError(); err != hipSuccess) return err;
+            }
         } else {
             err = gate_bwd_t<float>(c, s, dz, x, Wg, dx_in, dx, part, dbg_part, tc, nchunk);
         }
@@ -1156,8 +1166,9 @@ static hipError_t gate_bwd_contract(const Ctx& c, const evomoe_shape& s, const f
     if (err != hipSuccess) return err;
     const size_t n0 = (size_t)s.d * s.E, n1 = (size_t)s.E;
     ProfScope ps(c, EVOMOE_K_GATE_BWD_REDUCE);
-    hipLaunchKernelGGL(sum_chunks_kernel, dim3((n0 + n1 + 63) / 64), dim3(256), 0, c.stream, part, nchunk, n0,
-                       n1, dWg, dbg);
+    const size_t sums = (n0 + n1 + 63) / 64;
+    hipLaunchKernelGGL(sum_chunks_kernel, dim3((unsigned)(sums < kSumBlocks ? sums : kSumBlocks)), dim3(256), 0, c.stream, part, nchunk,
+                       n0, n1, dWg, dbg);
     return hipGetLastError();
 }
 

@@ -308,27 +308,33 @@ __global__ __launch_bounds__(256) void rmsnorm_dx_kernel(NormBwdArgs<TX> a)
 }
 
 // dgamma = the partial rows' sum.  Sixteen threads to a column, sixteen rows each at most (kParts), whose loads are all on their way at once;
-// their sums are added in order.
-constexpr int kParts = 256;
+// their sums are added in order.  A block has 64 columns at a time: a block for every 64 up to kSumBlocks (a grid dimension holds fewer
+// than 2^32 threads).
+constexpr int kParts = 256, kSumBlocks = 1 << 20;
 __global__ __launch_bounds__(1024) void dgamma_sum_kernel(const float* __restrict__ part, int parts, int d, float* __restrict__ dgamma)
 {
     __shared__ float sums[16][64];
-    const int o = threadIdx.x & 63, grp = threadIdx.x >> 6, i = blockIdx.x * 64 + o, per = (parts + 15) / 16;
-    float v[16];
+    const int o = threadIdx.x & 63, grp = threadIdx.x >> 6, per = (parts + 15) / 16;
+    for (int i0 = blockIdx.x * 64; i0 < d; i0 += gridDim.x * 64) {       // (d up to 2^30, a step up to 2^26)
+        const int i = i0 + o;
+        float v[16];
 #pragma unroll
-    for (int u = 0; u < 16; ++u) {
-        const int r = grp * per + u;
-        v[u] = u < per && r < parts && i < d ? part[(size_t)r * d + i] : 0.f;
+        for (int u = 0; u < 16; ++u) {
+            const int r = grp * per + u;
+            v[u] = u < per && r < parts && i < d ? part[(size_t)r * d + i] : 0.f;
+        }
+        float s = 0.f;
+#pragma unroll
+        for (int u = 0; u < 16; ++u) s += v[u];
+        sums[grp][o] = s;
+        __syncthreads();
+        if (grp == 0 && i < d) {
+#pragma unroll
+            for (int g = 1; g < 16; ++g) s += sums[g][o];
+            dgamma[i] = s;
+        }
+        __syncthreads();                             // (the sums have been read)
     }
-    float s = 0.f;
-#pragma unroll
-    for (int u = 0; u < 16; ++u) s += v[u];
-    sums[grp][o] = s;
-    __syncthreads();
-    if (grp > 0 || i >= d) return;
-#pragma unroll
-    for (int g = 1; g < 16; ++g) s += sums[g][o];
-    dgamma[i] = s;
 }
 
 // Rows of partial sums of dgamma: blocks of the one-pass kernel (sixteen rows each at least), or ranges of rows.
@@ -386,7 +392,7 @@ hipError_t add_rmsnorm_bwd_t(const Ctx& c, const evomoe_shape& s, const void* dy
     auto sum_up = [&] {
         const hipError_t err = hipGetLastError();
         if (err != hipSuccess || !dgamma) return err;
-        hipLaunchKernelGGL(dgamma_sum_kernel, dim3((s.d + 63) / 64), dim3(1024), 0, c.stream, a.part, a.parts, s.d, dgamma);
+        hipLaunchKernelGGL(dgamma_sum_kernel, dim3(std::min((s.d + 63) / 64, kSumBlocks)), dim3(1024), 0, c.stream, a.part, a.parts, s.d, dgamma);
         return hipGetLastError();
     };
     if (with_vectors<TX, 64 / KV>(s.d, [&](auto nv) {
