@@ -238,24 +238,34 @@ __global__ __launch_bounds__(256) void gate_prep_kernel(const float* __restrict_
                                                         uint16_t* __restrict__ planes, int32_t* __restrict__ counts,
                                                         int32_t* __restrict__ block_hist, int n_hist)
 {
-    const int i = blockIdx.x * 256 + threadIdx.x;          // over nkb * NE * 512 elements of one term, destination order
-    if (counts && i < E) counts[i] = 0;
-    if (block_hist && i < n_hist) block_hist[i] = 0;
+    // over nkb * NE * 512 elements of one term, destination order (which may be more than 2^31)
     const int nkb = (d + 31) / 32;
-    if (!planes || i >= nkb * NE * 512) return;
-    const int j = i & 7, lane = (i >> 3) & 63, n = (i >> 9) % NE, kb = (i >> 9) / NE;
-    const int e = n * 16 + (lane & 15), k = kb * 32 + (lane >> 4) * 8 + j;
-    const float w = (e < E && k < d) ? Wg[(size_t)k * E + e] : 0.f;
-    const uint32_t hi = f32_to_bf16_bits(w);
-    const float r1 = w - bf16_bits_to_f32(hi);
-    const uint32_t mid = f32_to_bf16_bits(r1);
-    const float r2 = r1 - bf16_bits_to_f32(mid);
-    const uint32_t lo = f32_to_bf16_bits(r2);
-    // element (kb, term, n, lane, j)
-    const size_t base = ((size_t)kb * 3 * NE + n) * 512 + (size_t)lane * 8 + j;
-    planes[base] = (uint16_t)hi;
-    planes[base + (size_t)NE * 512] = (uint16_t)mid;
-    planes[base + (size_t)2 * NE * 512] = (uint16_t)lo;
+    const uint32_t nb = planes ? (uint32_t)nkb * NE : 0;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;; i += (size_t)gridDim.x * 256) {
+        if (counts && i < (size_t)E) counts[i] = 0;
+        if (block_hist && i < (size_t)n_hist) block_hist[i] = 0;
+        const uint32_t b = (uint32_t)(i >> 9);
+        if (b >= nb) return;
+        const int j = i & 7, lane = (i >> 3) & 63, n = b % NE, kb = b / NE;
+        const int e = n * 16 + (lane & 15), k = kb * 32 + (lane >> 4) * 8 + j;
+        const float w = (e < E && k < d) ? Wg[(size_t)k * E + e] : 0.f;
+        const uint32_t hi = f32_to_bf16_bits(w);
+        const float r1 = w - bf16_bits_to_f32(hi);
+        const uint32_t mid = f32_to_bf16_bits(r1);
+        const float r2 = r1 - bf16_bits_to_f32(mid);
+        const uint32_t lo = f32_to_bf16_bits(r2);
+        // element (kb, term, n, lane, j)
+        const size_t base = ((size_t)kb * 3 * NE + n) * 512 + (size_t)lane * 8 + j;
+        planes[base] = (uint16_t)hi;
+        planes[base + (size_t)NE * 512] = (uint16_t)mid;
+        planes[base + (size_t)2 * NE * 512] = (uint16_t)lo;
+    }
+}
+// Blocks of gate_prep_kernel for `split` elements of one term (up to a cap: a grid dimension holds fewer than 2^32 threads) and `clear` words
+// that are cleared (fewer than the cap's).
+static unsigned prep_blocks(int64_t split, int clear) {
+    const int64_t a = (split + 255) / 256, cap = 1 << 20, b = (clear + 255) / 256;
+    return (unsigned)std::max(std::min(a, cap), b);
 }
 
 // SUB > 1 (one block, at most 16 experts): there is no split copy; every wave reads the float32 weights of its k-blocks
@@ -354,7 +364,7 @@ __global__ __launch_bounds__(256 * SUB) void dts_gate_bf16_kernel(
 
 hipError_t launch_clear_counts(const Ctx& c, const evomoe_shape& s, int32_t* counts, int32_t* block_hist) {
     const int n_hist = dispatch_blocks(s) * s.E, n = n_hist > s.E ? n_hist : s.E;
-    hipLaunchKernelGGL(gate_prep_kernel, dim3((n + 255) / 256), dim3(256), 0, c.stream, (const float*)nullptr, s.d, s.E, 0,
+    hipLaunchKernelGGL(gate_prep_kernel, dim3(prep_blocks(0, n)), dim3(256), 0, c.stream, (const float*)nullptr, s.d, s.E, 0,
                        (uint16_t*)nullptr, counts, block_hist, n_hist);
     return hipGetLastError();
 }
@@ -377,16 +387,14 @@ static hipError_t gate_launch_t(const Ctx& c, const evomoe_shape& s, const void*
     const int n_hist = dispatch_blocks(s) * s.E;
     ProfScope ps(c, EVOMOE_K_GATE);
     if constexpr (std::is_same<TX, bf16_t>::value) {
-        const int n_split = (s.d + 31) / 32 * NE * 512;
-        const int n = n_split > n_hist ? n_split : n_hist;
-        hipLaunchKernelGGL(gate_prep_kernel, dim3((n + 255) / 256), dim3(256), 0, c.stream, Wg, s.d, s.E, NE,
+        hipLaunchKernelGGL(gate_prep_kernel, dim3(prep_blocks(((int64_t)s.d + 31) / 32 * NE * 512, n_hist)), dim3(256), 0, c.stream, Wg, s.d, s.E, NE,
                            c.wg_planes, counts, block_hist, n_hist);
         hipLaunchKernelGGL((dts_gate_bf16_kernel<NE, RT>), dim3(blocks), dim3(256), 0, c.stream,
                            (const bf16_t*)x, (const bf16_t*)c.wg_planes, Wg, bg, noise, tau, thr, s.T, s.d, s.E,
                            gprime, gate_w, mask_bits, k_per_token, counts, block_hist);
     } else {
         const int n = n_hist > s.E ? n_hist : s.E;
-        hipLaunchKernelGGL(gate_prep_kernel, dim3((n + 255) / 256), dim3(256), 0, c.stream, Wg, s.d, s.E, 0,
+        hipLaunchKernelGGL(gate_prep_kernel, dim3(prep_blocks(0, n)), dim3(256), 0, c.stream, Wg, s.d, s.E, 0,
                            (uint16_t*)nullptr, counts, block_hist, n_hist);
         hipLaunchKernelGGL((dts_gate_kernel<TX, NE, RT>), dim3(blocks), dim3(256), 0, c.stream,
                            (const TX*)x, Wg, bg, noise, tau, thr, s.T, s.d, s.E, gprime, gate_w,
@@ -549,8 +557,7 @@ static hipError_t logits_launch_t(const Ctx& c, const evomoe_shape& s, const voi
     const int blocks = (s.T + 16 * RT - 1) / (16 * RT);
     ProfScope ps(c, EVOMOE_K_GATE_LOGITS);
     if constexpr (std::is_same<TX, bf16_t>::value) {
-        const int n = (s.d + 31) / 32 * NE * 512;
-        hipLaunchKernelGGL(gate_prep_kernel, dim3((n + 255) / 256), dim3(256), 0, c.stream, Wg, s.d, s.E, NE,
+        hipLaunchKernelGGL(gate_prep_kernel, dim3(prep_blocks(((int64_t)s.d + 31) / 32 * NE * 512, 0)), dim3(256), 0, c.stream, Wg, s.d, s.E, NE,
                            c.wg_planes, (int32_t*)nullptr, (int32_t*)nullptr, 0);
         hipLaunchKernelGGL((dts_gate_bf16_kernel<NE, RT, 1, true>), dim3(blocks), dim3(256), 0, c.stream, (const bf16_t*)x,
                            (const bf16_t*)c.wg_planes, Wg, bg, (const float*)nullptr, 1.f, 0.f, s.T, s.d, s.E, logits,

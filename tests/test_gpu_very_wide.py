@@ -85,3 +85,22 @@ def test_logits_of_wide_rows(ctx, dtype):
         assert ((dx[:, c] - want).abs() <= (rough + 2 * E * U) * mag + step * want.abs()).all(), c
     assert ((z - sums).abs() <= (d / 16 + 20) * U * size).all()
     assert ((dbg - zd.sum(0)).abs() <= 4 * U * zd.abs().sum(0)).all()
+
+
+def test_gate_of_a_wide_bf16_layer(ctx):
+    """The split copy of W_g has more than 2^31 elements to a term.  x of -1 and 1, W_g of -1, 0 and 1 times 2^-12: every sum is exact."""
+    T, d, E = 1, (1 << 25) + 64, 64
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randint(0, 2, (T, d), generator=g, device="cuda").mul_(2).sub_(1).to(torch.bfloat16)
+    Wg = torch.randint(-1, 2, (d, E), generator=g, device="cuda", dtype=torch.int8).float().mul_(2.0 ** -12)
+    gp, gw = torch.empty(T, E, device="cuda"), torch.empty(T, E, device="cuda")
+    mask, counts = torch.empty(T, dtype=torch.int64, device="cuda"), torch.empty(E, dtype=torch.int32, device="cuda")
+    B.evomoe_dts_gate(ctx, B.make_shape(T, d, E, 8, "bf16", "relu", E), x, Wg, None, None, 1.0, 0.01, gp, gw, mask, counts, None)
+    torch.cuda.synchronize()
+    z = torch.zeros(T, E, dtype=torch.float64, device="cuda")
+    for c in runs(d):
+        z += x[:, c].double() @ Wg[c].double()
+    want = torch.softmax(z, 1)
+    # softmax: the argument z - max, of up to 8, is rounded once (8 U), the exponential, a sum of 64 terms and the quotient take 24 more
+    assert float((z.max() - z.min())) < 8
+    assert ((gp - want).abs() <= 32 * U * want).all(), (gp, want)
