@@ -1,4 +1,6 @@
 // C ABI of the DTS-Gate MoE layer: argument validation, context, and hand-off to the kernel launchers.
+#include <algorithm>
+#include <initializer_list>
 #include <new>
 
 #include "kernels.h"
@@ -82,6 +84,9 @@ evomoe_status check_topk(const evomoe_topk* o, int E) {
         CHECK_CTX_SHAPE();                                          \
         if (shape->T > (1 << 29) || shape->d > (1 << 30)) return EVOMOE_EUNSUPPORTED; \
     } while (0)
+
+// one workspace for several calls, in whole 256 bytes
+size_t largest(std::initializer_list<size_t> bytes) { return (std::max(bytes) + 255) & ~(size_t)255; }
 
 evomoe_status from_hip(hipError_t e) { return e == hipSuccess ? EVOMOE_OK : EVOMOE_EHIP; }
 
@@ -190,10 +195,8 @@ const char* evomoe_status_string(evomoe_status s) {
 
 size_t evomoe_workspace_bytes(const evomoe_shape* shape) {
     if (check_shape(shape) != EVOMOE_OK) return 0;
-    const size_t a = ffn_bwd_workspace_bytes(*shape), b = gate_bwd_workspace_bytes(*shape),
-                 n = rmsnorm_bwd_workspace_bytes(*shape);
-    const size_t m = a > b ? a : b;
-    return ((m > n ? m : n) + 255) & ~(size_t)255;
+    return largest({ffn_bwd_workspace_bytes(*shape), gate_bwd_workspace_bytes(*shape), logits_bwd_workspace_bytes(*shape),
+                    rmsnorm_bwd_workspace_bytes(*shape)});
 }
 
 evomoe_status evomoe_dts_gate(evomoe_ctx* ctx, const evomoe_shape* shape, const void* x,
@@ -357,9 +360,7 @@ evomoe_status evomoe_dts_gate_bwd_balance(evomoe_ctx* ctx, const evomoe_shape* s
 
 size_t evomoe_workspace_bytes_recompute(const evomoe_shape* shape) {
     if (check_shape(shape) != EVOMOE_OK) return 0;
-    const size_t a = ffn_bwd_recompute_workspace_bytes(*shape), b = gate_bwd_workspace_bytes(*shape);
-    const size_t m = a > b ? a : b;
-    return (m + 255) & ~(size_t)255;
+    return largest({ffn_bwd_recompute_workspace_bytes(*shape), gate_bwd_workspace_bytes(*shape), logits_bwd_workspace_bytes(*shape)});
 }
 
 evomoe_status evomoe_expert_ffn_bwd_recompute(evomoe_ctx* ctx, const evomoe_shape* shape, const void* dO,
@@ -450,7 +451,7 @@ evomoe_status evomoe_gate_logits_bwd(evomoe_ctx* ctx, const evomoe_shape* shape,
     CHECK_CTX_BLOCK();
     REQUIRE_PTR(dlogits); REQUIRE_PTR(x); REQUIRE_PTR(Wg); REQUIRE_PTR(dWg); REQUIRE_PTR(dx);
     OPTIONAL_PTR(dx_in); OPTIONAL_PTR(dbg);
-    if (!workspace || !aligned16(workspace) || workspace_bytes < gate_bwd_workspace_bytes(*shape))
+    if (!workspace || !aligned16(workspace) || workspace_bytes < logits_bwd_workspace_bytes(*shape))
         return EVOMOE_EWORKSPACE;
     ON_DEVICE();
     return from_hip(launch_gate_logits_bwd(ctx->c, *shape, dlogits, x, Wg, dx_in, dWg, dbg, dx, (float*)workspace));

@@ -1100,12 +1100,16 @@ static int gate_bwd_chunk_tokens(const evomoe_shape& s) {
     return tc;
 }
 
+// [partial tables of dW_g, db_g: one to a chunk of tokens]
+static size_t tables_bytes(const evomoe_shape& s, size_t n) { return n * ((size_t)s.d * s.E + s.E) * sizeof(float); }
+// DTS gate: [dz: T x E][tables of that path's plan]
 size_t gate_bwd_workspace_bytes(const evomoe_shape& s) {
     const int tc = gate_bwd_chunk_tokens(s);
-    size_t nchunk = (s.T + tc - 1) / tc;
-    if (gate_bwd_use_mfma(s)) nchunk = gate_bwd_mfma_plan(s).nblk;
-    else if ((size_t)logits_bwd_f32_plan(s).nblk > nchunk) nchunk = logits_bwd_f32_plan(s).nblk;
-    return ((size_t)s.T * s.E + nchunk * ((size_t)s.d * s.E + s.E)) * sizeof(float);
+    const size_t n = gate_bwd_use_mfma(s) ? gate_bwd_mfma_plan(s).nblk : ((size_t)s.T + tc - 1) / tc;
+    return (size_t)s.T * s.E * sizeof(float) + tables_bytes(s, n);
+}
+size_t logits_bwd_workspace_bytes(const evomoe_shape& s) {
+    return tables_bytes(s, gate_bwd_use_mfma(s) ? gate_bwd_mfma_plan(s).nblk : logits_bwd_f32_plan(s).nblk);
 }
 
 template <typename TX>

@@ -14,11 +14,12 @@ hipError_t launch_dts_gate_bwd(const Ctx& c, const evomoe_shape& s, const float*
                                const uint64_t* mask_bits, float tau, const void* x, const float* Wg,
                                float* dWg, float* dbg, void* dx, void* workspace,
                                const float* dgprime_coef = nullptr, float coef_scale = 0.f);
-size_t gate_bwd_workspace_bytes(const evomoe_shape& s);
+size_t gate_bwd_workspace_bytes(const evomoe_shape& s);        // of the DTS gate
+size_t logits_bwd_workspace_bytes(const evomoe_shape& s);      // of the logits alone
 bool gate_logits_use_planes(const Ctx& c, const evomoe_shape& s);      // whether launch_gate_logits needs the split copy of W_g
 hipError_t launch_gate_logits(const Ctx& c, const evomoe_shape& s, const void* x, const float* Wg, const float* bg,
                               float* logits);
-// part: gate_bwd_workspace_bytes(s) hold it
+// part: logits_bwd_workspace_bytes(s) hold it
 hipError_t launch_gate_logits_bwd(const Ctx& c, const evomoe_shape& s, const float* dz, const void* x, const float* Wg,
                                   const void* dx_in, float* dWg, float* dbg, void* dx, float* part);
 // clears counts [E] and block_hist (may be null)
