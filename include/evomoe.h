@@ -240,7 +240,7 @@ evomoe_status evomoe_dts_gate_bwd_balance(evomoe_ctx* ctx, const evomoe_shape* s
  * Costs 14*d*F instead of 12*d*F flop per pair over forward + backward and saves 2*P_cap*F elements of
  * resident activations.  Arguments as evomoe_expert_ffn_bwd without H and A, plus b1 (dy and pair_gate optional,
  * as there).
- *   workspace: at least evomoe_workspace_bytes_recompute(shape) bytes. */
+ *   workspace: at least evomoe_workspace_bytes_recompute(shape) bytes, which is enough for the block's other backward passes too. */
 size_t evomoe_workspace_bytes_recompute(const evomoe_shape* shape);
 evomoe_status evomoe_expert_ffn_bwd_recompute(evomoe_ctx* ctx, const evomoe_shape* shape,
                                               const void* dO,

@@ -360,7 +360,8 @@ evomoe_status evomoe_dts_gate_bwd_balance(evomoe_ctx* ctx, const evomoe_shape* s
 
 size_t evomoe_workspace_bytes_recompute(const evomoe_shape* shape) {
     if (check_shape(shape) != EVOMOE_OK) return 0;
-    return largest({ffn_bwd_recompute_workspace_bytes(*shape), gate_bwd_workspace_bytes(*shape), logits_bwd_workspace_bytes(*shape)});
+    return largest({ffn_bwd_recompute_workspace_bytes(*shape), gate_bwd_workspace_bytes(*shape), logits_bwd_workspace_bytes(*shape),
+                    rmsnorm_bwd_workspace_bytes(*shape)});
 }
 
 evomoe_status evomoe_expert_ffn_bwd_recompute(evomoe_ctx* ctx, const evomoe_shape* shape, const void* dO,
