@@ -379,9 +379,10 @@ evomoe_status evomoe_add_rmsnorm_bwd(evomoe_ctx* ctx, const evomoe_shape* shape,
 evomoe_status evomoe_quantize_mx8(evomoe_ctx* ctx, int64_t rows, int64_t cols, int dtype,
                                   const void* src, void* q, uint8_t* q_scale);
 
-/* Expert FFNs forward in 8 bits, for serving a bf16 layer: evomoe_expert_ffn with x, W1, W2 and act(H) as 8-bit values, products
- * on the scaled matrix instructions, sums, biases and activation in float32.  act(H) is converted in float32 and stays in
- * the workspace.
+/* Expert FFNs forward in 8 bits, for serving a bf16 layer: evomoe_expert_ffn with x, W1, W2 and act(H) as 8-bit values.
+ * Products on the scaled matrix instructions: of eight neighbours along the contraction (8 i .. 8 i + 7) each product is cut off below 2^-13 of
+ * 2^(the largest sum of two factors' exponents); the sums of eight are added in float32, and biases (and an activation within 7e-7 of
+ * the exact one) are float32's.  act(H) is converted from float32 and stays in the workspace.
  *   in : x_q [T,d], x_scale [T,d/32], gathered through pair_token [P_cap], or, if pair_token == NULL, permuted rows
  *        [P_cap,d]; expert_offsets [E+1]; W1_q [E,F,d], W1_scale [E,F,d/32], b1 [E,F] f32 (NULL = 0), W2_q [E,d,F],
  *        W2_scale [E,d,F/32], b2 [E,d] f32 (NULL = 0).

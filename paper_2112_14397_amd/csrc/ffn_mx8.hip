@@ -29,8 +29,9 @@ struct Mx8Args {
     int64_t P_cap;
 };
 
-// gelu(h) = max(h, 0) - x 2^p(x), x = |h|: 2^p is Phi(-x), p of degree five fitted for the least largest error of the product,
-// 5e-7 with float32's own, for every finite h (p falls to -inf).  Ten VALU instructions and an exponential.
+// gelu(h) = max(h, 0) - x 2^p(x), x = |h|: 2^p is Phi(-x), p of degree five fitted for the least largest error of the product.  For every
+// finite h (p falls to -inf) the value is within 4.7e-7 and half a float32 step of itself of the exact one, 6.4e-7 at most (near h = 4).
+// Ten VALU instructions and an exponential.
 __device__ __forceinline__ float gelu5(float h) {
     const float x = fabsf(h);
     float p = -0.000473309294f;
