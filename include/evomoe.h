@@ -288,6 +288,8 @@ evomoe_status evomoe_diversify(evomoe_ctx* ctx, const evomoe_shape* shape,
 
 /* Gate logits:  logits[t,:] = x_t . W_g + b_g.
  *   in : x [T,d] elem; Wg [d,E] f32; bg [E] f32 or NULL.   out: logits [T,E] f32.
+ * Products are exact (bf16) or float32's, sums float32's.  The order of a sum over d, and with it a logit's last bits, depends on T: of up to
+ * sixteen tokens for each compute unit (4096 of 256; in float32 with d from 512 on five times as many) it is another one than of more.
  * F and P_cap of the shape are not used. */
 evomoe_status evomoe_gate_logits(evomoe_ctx* ctx, const evomoe_shape* shape,
                                  const void* x, const float* Wg, const float* bg, float* logits);
@@ -308,7 +310,8 @@ evomoe_status evomoe_gate_logits_bwd(evomoe_ctx* ctx, const evomoe_shape* shape,
  * selected.  Ties go to the lowest index.  The bias decides the selection alone: the weight of a selected expert is
  *     w_i = scale * s_i        or, renormalised,     w_i = scale * s_i / sum of s over the token's selected experts.
  * Keys are compared as 64-bit values of the float32 logits (with no bias and one group, the logits themselves are), so
- * the selection depends neither on the rounding of an exponential nor on the batch that a token is in.
+ * the selection of given logits depends neither on the rounding of an exponential nor on the batch that a token is in.  (The logits'
+ * own last bits may: see evomoe_gate_logits.)
  *  - A logit or a bias of -inf takes the expert out: it is not selected, and a logit of -inf has the score 0.  A token with fewer
  *    than k experts left selects those, one with none (padding) selects nothing: k_s = 0, and the layer's output is 0.
  *  - A NaN key ranks above every number, so that a NaN reaches the output; so do the NaNs of a softmax over +inf.  */
