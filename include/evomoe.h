@@ -298,6 +298,7 @@ evomoe_status evomoe_gate_logits(evomoe_ctx* ctx, const evomoe_shape* shape,
  *   in : dlogits [T,E] f32, x, Wg as in the forward; dx_in [T,d] elem (what else flows into x, for instance the output of
  *        evomoe_dispatch_bwd; NULL = 0).
  *   out: dWg [d,E] f32, dbg [E] f32 (may be NULL), dx [T,d] elem; dx may be dx_in itself.
+ * dx of a bf16 layer takes W_g and dlogits to 16 bits each: off by up to 2^-16 of the magnitudes, beside its rounding to bf16.
  *   workspace: at least evomoe_workspace_bytes(shape) bytes. */
 evomoe_status evomoe_gate_logits_bwd(evomoe_ctx* ctx, const evomoe_shape* shape,
                                      const float* dlogits, const void* x, const float* Wg, const void* dx_in,

@@ -92,7 +92,8 @@ __device__ __forceinline__ void store4(float* to, bool there, size_t at, int e0,
     }
 }
 
-// Scores in float32; rest = 1 - s of a sigmoid
+// Scores in float32; rest = 1 - s of a sigmoid.  The reciprocals, here and of the weights, are the instruction's, within one step of float32
+// where a division is within half of one; key_margin counts it, and no output is narrower than that.
 template <int LPT> __device__ __forceinline__ void scores_of(const float (&z)[4], bool softmax, float (&s)[4], float (&rest)[4]) {
     if (softmax) {
         float m = lanes_max<LPT>(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]))), sum = 0.f;
