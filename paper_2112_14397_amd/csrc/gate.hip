@@ -238,15 +238,18 @@ __global__ __launch_bounds__(256) void gate_prep_kernel(const float* __restrict_
                                                         uint16_t* __restrict__ planes, int32_t* __restrict__ counts,
                                                         int32_t* __restrict__ block_hist, int n_hist)
 {
-    // over nkb * NE * 512 elements of one term, destination order (which may be more than 2^31)
-    const int nkb = (d + 31) / 32;
-    const uint32_t nb = planes ? (uint32_t)nkb * NE : 0;
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;; i += (size_t)gridDim.x * 256) {
-        if (counts && i < (size_t)E) counts[i] = 0;
-        if (block_hist && i < (size_t)n_hist) block_hist[i] = 0;
-        const uint32_t b = (uint32_t)(i >> 9);
+    // over nkb * NE * 512 elements of one term, destination order: they may be more than 2^32, their blocks of 256 are not
+    const uint32_t nb = planes ? (uint32_t)((d + 31) / 32) * NE : 0;
+    for (uint32_t blk = blockIdx.x;; blk += gridDim.x) {
+        if (blk < (1u << 16)) {                      // (the words that are cleared are fewer than 2^24)
+            const int i = blk * 256 + threadIdx.x;
+            if (counts && i < E) counts[i] = 0;
+            if (block_hist && i < n_hist) block_hist[i] = 0;
+        }
+        const uint32_t b = blk >> 1;
         if (b >= nb) return;
-        const int j = i & 7, lane = (i >> 3) & 63, n = b % NE, kb = b / NE;
+        const uint32_t i = (blk & 1) * 256 + threadIdx.x;
+        const int j = i & 7, lane = i >> 3, n = b % NE, kb = b / NE;
         const int e = n * 16 + (lane & 15), k = kb * 32 + (lane >> 4) * 8 + j;
         const float w = (e < E && k < d) ? Wg[(size_t)k * E + e] : 0.f;
         const uint32_t hi = f32_to_bf16_bits(w);
